@@ -64,7 +64,8 @@ typedef enum { M2RNN_F32 = 0, M2RNN_BF16 = 1 } m2rnn_dtype;
 typedef enum {
   M2RNN_GATE_VALUE = 0, /* gate tensor IS f_t in [0,1]                 (Algorithm 1, input F)    */
   M2RNN_GATE_LOGIT = 1, /* f_t = 1/(1+exp(-gate))                      (forget-gate eq., alpha=1, beta=0, x=-gate) */
-  M2RNN_GATE_PSI = 2    /* f_t = (1+exp(gate+beta_n))^(-alpha_n)       (forget-gate equation)    */
+  M2RNN_GATE_PSI = 2,   /* f_t = (1+exp(gate+beta_n))^(-alpha_n)       (forget-gate equation)    */
+  M2RNN_GATE_LOG = 3    /* f_t = exp(gate): the gated delta rule's calls only (below)            */
 } m2rnn_gate_kind;
 
 typedef struct {
@@ -278,6 +279,95 @@ int m2rnn_conv_silu_bwd(int32_t B, int32_t T, int32_t C, int32_t io_dtype, const
                         const void *w, const void *bias, const void *prev, const void *dout,
                         int64_t dout_stride, void *dx, int64_t dx_stride, float *dw, float *dbias,
                         void *dprev, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- Gated delta rule: the linear recurrence of the layers that an M2RNN layer stands among in the paper's hybrid
+ * models ("Hybrid GDN": gated delta net).  Per (b, n), on a K x V state H, with a decay a_t and a step b_t:
+ *     u_t = b_t (v_t - a_t H_{t-1}^T k_t)      H_t = a_t H_{t-1} + k_t u_t^T      y_t = q_scale H_t^T q_t
+ * Layouts, head groups, token strides, packed batches and conventions are those of the scan calls above, with these
+ * differences: gate and step have the element type io_dtype (they come out of a projection, like v); the states have a
+ * type of their own, state_dtype; there is no W.
+ * a_t comes from the gate tensor by gate_kind: M2RNN_GATE_LOG a = exp(gate) (gate <= 0; -inf: the state is dropped),
+ * M2RNN_GATE_LOGIT, M2RNN_GATE_PSI as above.  (M2RNN_GATE_VALUE is refused: the kernels and the gradient work on log a.)
+ * b_t comes from the step tensor by step_kind.  A token with a = 1 and b = 0 leaves the state as it is.
+ * With M2RNN_BF16 the sequence is taken in chunks of 32 tokens whose products run on tensor cores: bf16 operands (the
+ * state's included), fp32 accumulation, the state itself held in fp32.  Outputs of fp32 type (a state_dtype of
+ * M2RNN_F32) then carry the error of those operands, some 3e-3 of their norm.  With M2RNN_F32 everything is fp32 FMA.
+ * Supported sizes: K a multiple of 16 in 16..128, V in {16,32,64,128}. */
+typedef enum {
+  M2RNN_STEP_VALUE = 0, /* step tensor IS b_t            */
+  M2RNN_STEP_LOGIT = 1  /* b_t = 1/(1+exp(-step))        */
+} m2rnn_step_kind;
+
+typedef struct {
+  int32_t B, T, N, Nq, Nk, K, V; /* as in m2rnn_params */
+  int32_t io_dtype;      /* m2rnn_dtype of q, k, v, gate, step, y, dy and all gradients but dh0 */
+  int32_t state_dtype;   /* m2rnn_dtype of h0, hT, d_hT, dh0 and the decoding step's states     */
+  int32_t gate_kind;     /* M2RNN_GATE_LOG, _LOGIT or _PSI                                      */
+  int32_t step_kind;     /* m2rnn_step_kind                                                     */
+  int32_t qk_norm;       /* != 0: q_t and k_t are divided by sqrt(their sum of squares + norm_eps) */
+  float norm_eps, q_scale;
+  int64_t q_stride, k_stride, v_stride, total_tokens; /* as in m2rnn_params */
+  const int32_t *cu_seqlens;                          /* as in m2rnn_params */
+} m2rnn_delta_params;
+
+/* Bytes of `ckpt`, what a forward call leaves for the backward call (opaque; 256-byte aligned). */
+size_t m2rnn_delta_ckpt_bytes(const m2rnn_delta_params *params);
+
+/* Scratch of the forward call; `have_ckpt` != 0 if it will be given a ckpt. */
+size_t m2rnn_delta_fwd_workspace_bytes(const m2rnn_delta_params *params, int have_ckpt);
+
+/* Forward pass over whole sequences (T from 1 up).
+ *   in : q [B,T,Nq,K], k [B,T,Nk,K], v [B,T,N,V], gate, step [B,T,N]; h0 [B,N,K,V] or NULL (zeros); alpha, beta [N]
+ *        fp32 (M2RNN_GATE_PSI only, else ignored)
+ *   out: y [B,T,N,V]; hT [B,N,K,V] or NULL; ckpt or NULL
+ * T = 0, B = 0 and a batch without tokens are valid empty calls: nothing is written (as for m2rnn_fwd).  An empty
+ * sequence of a packed batch has hT = h0. */
+int m2rnn_delta_fwd(const m2rnn_delta_params *params, const void *q, const void *k, const void *v, const void *gate,
+                    const void *step, const void *h0, const float *alpha, const float *beta, void *y, void *hT,
+                    void *ckpt, void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/* Scratch of the backward call; `have_ckpt` != 0 if it will be given the forward call's ckpt. */
+size_t m2rnn_delta_bwd_workspace_bytes(const m2rnn_delta_params *params, int have_ckpt);
+
+/* Gradients.
+ *   in : the forward inputs; ckpt as a forward call with the same params and inputs left it, or NULL (recomputed);
+ *        dy [B,T,N,V]; d_hT [B,N,K,V] or NULL
+ *   out: dq, dk (summed over the heads that share them), dv, dgate, dstep (w.r.t. the tensors as passed), all dense and
+ *        of io_dtype; dh0 or NULL.  Sums are taken in a fixed order: results repeat bit for bit.
+ * The gradients of alpha and beta are elementwise sums of dgate outside the call (d beta_n = sum dgate,
+ * d alpha_n = sum dgate softplus(x) / (alpha sigmoid(x)), x = gate + beta_n). */
+int m2rnn_delta_bwd(const m2rnn_delta_params *params, const void *q, const void *k, const void *v, const void *gate,
+                    const void *step, const void *h0, const float *alpha, const float *beta, const void *ckpt,
+                    const void *dy, const void *d_hT, void *dq, void *dk, void *dv, void *dgate, void *dstep, void *dh0,
+                    void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/* One decoding step on cached states (params->T, strides and cu_seqlens are ignored; all arithmetic is fp32).
+ *   in : q [B,Nq,K], k [B,Nk,K], v [B,N,V], gate, step [B,N]; slots [B] (device) or NULL: row b's state is
+ *        state[slots[b]], or state[b] (n_slots = B then)
+ *   io : state [n_slots,N,K,V], updated in place; other slots are left alone
+ *   out: y [B,N,V]
+ * The slots of the rows are distinct (of a slot that comes twice the state and the rows' y are undefined).  A negative
+ * slot marks a padding row: no state is touched, its y is 0.  So for a slot >= n_slots, which also stores
+ * M2RNN_ERR_SHAPE in *dev_status. */
+int m2rnn_delta_decode_step(const m2rnn_delta_params *params, const void *q, const void *k, const void *v,
+                            const void *gate, const void *step, const float *alpha, const float *beta, void *state,
+                            const int32_t *slots, int32_t n_slots, void *y, int32_t *dev_status, void *stream);
+
+/* ---- States of a cache moved between its slots: copied, forked, compacted, freed.
+ *     dst[layer][dst_slots[i]] = src[layer][src_slots[i]]      for all i < n at once, in every layer
+ * as if every source were read before any destination is written: dst and src may be the same cache, and a slot both a
+ * source and a destination (shifts, swaps).  A source may come several times (a fork).  A negative source stands for
+ * zeros (a freed or fresh slot), a negative destination leaves the pair out; of a destination that comes twice the
+ * last pair counts.  A slot outside its cache leaves the pair out and stores M2RNN_ERR_SHAPE in *dev_status.
+ * The paper has no counterpart.  It serves every kind of state: m2rnn_decode_step's [B,N,K,V], the delta rule's, the
+ * rows that the convolution carries.
+ *   dst, src : device; `rows` rows of `row_bytes` (a multiple of 16) to a layer, layers `layer_stride` bytes apart
+ *              (ignored for one layer); either the same memory or apart
+ *   dst_slots, src_slots : device int32 [n], n at most m2rnn_state_copy_limit() */
+int m2rnn_state_copy_limit(void);
+int m2rnn_state_copy(void *dst, const int32_t *dst_slots, int32_t dst_rows, int64_t dst_layer_stride, const void *src,
+                     const int32_t *src_slots, int32_t src_rows, int64_t src_layer_stride, int32_t n,
+                     int64_t row_bytes, int32_t layers, int32_t *dev_status, void *stream);
 
 #ifdef __cplusplus
 }

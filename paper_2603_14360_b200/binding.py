@@ -11,6 +11,10 @@ the GPU, so its host path is what counts.  The size queries and self-tests go th
     y1          = m2rnn_decode_step(q1, k1, v1, gate1, W, state)      # state updated in place
     out, rstd   = m2rnn_gated_norm_fwd(y, g_in, w)                    # RMSNorm(y * SiLU(g)) over N*V
     grads       = m2rnn_gated_norm_bwd(y, g_in, w, rstd, dout)        # dy, dg, dw
+    y, hT, ckpt = m2rnn_delta_fwd(q, k, v, gate, step, h0, save_ckpt=True)       # gated delta rule
+    grads       = m2rnn_delta_bwd(q, k, v, gate, step, h0, dy, ckpt=ckpt)
+    y1          = m2rnn_delta_decode_step(q1, k1, v1, gate1, step1, pool, slots=slots)
+    m2rnn_state_copy(pool, dst_slots, src_slots)                      # states forked, moved, cleared
 
 Tensor layouts are the paper's (Algorithm 1/2): q [B,T,Nq,K], k [B,T,Nk,K], v [B,T,N,V],
 gate [B,T,N] fp32, W [N,V,V], h0 [B,N,K,V] fp32.
@@ -22,7 +26,8 @@ import os
 
 import torch
 
-GATE_VALUE, GATE_LOGIT, GATE_PSI = 0, 1, 2
+GATE_VALUE, GATE_LOGIT, GATE_PSI, GATE_LOG = 0, 1, 2, 3
+STEP_VALUE, STEP_LOGIT = 0, 1
 F32, BF16 = 0, 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -49,9 +54,19 @@ class Params(ctypes.Structure):
                 ("total_tokens", ctypes.c_int64), ("cu_seqlens", ctypes.c_void_p)]
 
 
+class DeltaParams(ctypes.Structure):
+    """Mirror of ``m2rnn_delta_params``."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "T", "N", "Nq", "Nk", "K", "V", "io_dtype", "state_dtype", "gate_kind",
+                                              "step_kind", "qk_norm")]
+    _fields_ += [("norm_eps", ctypes.c_float), ("q_scale", ctypes.c_float),
+                 ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                 ("total_tokens", ctypes.c_int64), ("cu_seqlens", ctypes.c_void_p)]
+
+
 _LIB = None
 _vp = ctypes.c_void_p
 _pp = ctypes.POINTER(Params)
+_dp = ctypes.POINTER(DeltaParams)
 
 EXPORTS = {
     "m2rnn_version": (ctypes.c_int, []),
@@ -75,6 +90,15 @@ EXPORTS = {
     "m2rnn_gated_norm_bwd_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64, ctypes.c_int32]),
     "m2rnn_gated_norm_bwd": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _vp, _vp, _vp, _vp, ctypes.c_int32,
                                             _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
+    "m2rnn_delta_ckpt_bytes": (ctypes.c_size_t, [_dp]),
+    "m2rnn_delta_fwd_workspace_bytes": (ctypes.c_size_t, [_dp, ctypes.c_int]),
+    "m2rnn_delta_fwd": (ctypes.c_int, [_dp] + [_vp] * 12 + [ctypes.c_size_t, _vp, _vp]),
+    "m2rnn_delta_bwd_workspace_bytes": (ctypes.c_size_t, [_dp, ctypes.c_int]),
+    "m2rnn_delta_bwd": (ctypes.c_int, [_dp] + [_vp] * 18 + [ctypes.c_size_t, _vp, _vp]),
+    "m2rnn_delta_decode_step": (ctypes.c_int, [_dp] + [_vp] * 9 + [ctypes.c_int32, _vp, _vp, _vp]),
+    "m2rnn_state_copy_limit": (ctypes.c_int, []),
+    "m2rnn_state_copy": (ctypes.c_int, [_vp, _vp, ctypes.c_int32, ctypes.c_int64, _vp, _vp, ctypes.c_int32, ctypes.c_int64,
+                                        ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, _vp, _vp]),
 }
 
 STATIC_SCRATCH_BYTES = 8 << 20   # M2RNN_STATIC_SCRATCH_BYTES
@@ -319,3 +343,48 @@ def m2rnn_conv_silu_bwd(x, w, dout, bias=None, prev=None, *, out=None, workspace
     if dprev is not None:
         res["dprev"] = dprev
     return res
+
+
+def m2rnn_delta_fwd(q, k, v, gate, step, h0=None, *, gate_kind=GATE_LOG, alpha=None, beta=None, step_kind=STEP_VALUE,
+                    qk_norm=False, norm_eps=1e-6, q_scale=1.0, save_ckpt=False, want_hT=True, state_dtype=None, out=None,
+                    workspace=None, stream=None, cu_seqlens=None, max_seqlen=None):
+    """Gated delta rule over whole sequences: u = b (v - a H^T k), H = a H + k u^T, y = q_scale H^T q.
+    q [B,T,Nq,K], k [B,T,Nk,K], v [B,T,N,V], gate and step [B,T,N], all of one type (bf16 or fp32); the decay
+    a comes from ``gate`` by ``gate_kind`` (GATE_LOG: a = exp(gate); GATE_LOGIT; GATE_PSI with alpha, beta [N] fp32),
+    the step b from ``step`` by ``step_kind``.  ``qk_norm``: q and k are divided by their lengths first.
+    h0 and hT [B,N,K,V] have the type of h0 (else ``state_dtype``, else fp32).  Strides, packed batches, ``out`` and
+    ``workspace`` as in ``m2rnn_fwd``.  Returns (y, hT, ckpt); ``ckpt`` (``save_ckpt``) is for ``m2rnn_delta_bwd``."""
+    y, hT, ckpt = (out.get("y"), out.get("hT"), out.get("ckpt")) if out else (None, None, None)
+    return _native.delta_fwd(q, k, v, gate, step, h0, gate_kind, alpha, beta, step_kind, qk_norm, norm_eps, q_scale, save_ckpt,
+                             want_hT, state_dtype is not None and _io_code(state_dtype) == BF16, y, hT, ckpt, workspace, stream,
+                             cu_seqlens, max_seqlen)
+
+
+def m2rnn_delta_bwd(q, k, v, gate, step, h0, dy, d_hT=None, *, ckpt=None, gate_kind=GATE_LOG, alpha=None, beta=None,
+                    step_kind=STEP_VALUE, qk_norm=False, norm_eps=1e-6, q_scale=1.0, want_dh0=True, state_dtype=None,
+                    workspace=None, out=None, stream=None, cu_seqlens=None, max_seqlen=None):
+    """Backward of ``m2rnn_delta_fwd`` -> dict(dq, dk, dv, dgate, dstep, dh0), dense, of the inputs' type (dh0: the
+    states').  ``ckpt`` as the forward call with the same inputs and options returned it; without it the forward pass
+    is recomputed."""
+    dq, dk, dv, dgate, dstep, dh0 = map(out.get, ("dq", "dk", "dv", "dgate", "dstep", "dh0")) if out else (None,) * 6
+    return _native.delta_bwd(q, k, v, gate, step, h0, gate_kind, alpha, beta, step_kind, qk_norm, norm_eps, q_scale, dy, d_hT, ckpt,
+                             want_dh0, state_dtype is not None and _io_code(state_dtype) == BF16, workspace, dq, dk, dv, dgate, dstep,
+                             dh0, stream, cu_seqlens, max_seqlen)
+
+
+def m2rnn_delta_decode_step(q, k, v, gate, step, state, *, slots=None, gate_kind=GATE_LOG, alpha=None, beta=None,
+                            step_kind=STEP_VALUE, qk_norm=False, norm_eps=1e-6, q_scale=1.0, y=None, stream=None):
+    """One token of the gated delta rule on cached states (fp32 or bf16), updated in place: ``state`` [B,N,K,V], or a
+    pool [S,N,K,V] of which row b uses slot ``slots[b]`` (int32, distinct; negative: a padding row, y = 0).
+    Returns y [B,N,V]."""
+    return _native.delta_decode_step(q, k, v, gate, step, state, gate_kind, alpha, beta, step_kind, qk_norm, norm_eps, q_scale, slots,
+                                     y, stream)
+
+
+def m2rnn_state_copy(dst, dst_slots, src_slots, src=None, *, axis=0, stream=None):
+    """dst[dst_slots[i]] = src[src_slots[i]] along ``axis`` (axes before it are layers) for all i at once: sources are
+    read before destinations are written, also where ``src`` is ``dst`` (the default).  Slots are int32 tensors; a
+    negative source clears, a negative destination leaves the pair out, of a repeated destination the last counts.
+    For the states of any call here, e.g. a pool [S,N,K,V] or, for all layers at once, [layers,S,N,K,V] with axis=1.
+    Returns dst."""
+    return _native.state_copy(dst, dst_slots, src_slots, src, axis, stream)

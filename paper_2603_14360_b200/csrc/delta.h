@@ -1,0 +1,111 @@
+// Internal declarations of the gated delta rule (delta_*.cu) and of the state copy.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "m2rnn.h"
+
+namespace m2rnn {
+
+constexpr int kDeltaChunk = 32;        // tokens of a chunk (bf16 kernels)
+constexpr int kDeltaChunkF32 = 16;     // (fp32 kernels)
+
+// What the chains and the gradient kernel need of one chunk of one head (delta_prep.cu):
+//   T, P: 32 x 32 bf16 as 8 x 8 blocks, block (bi, bj) at 128 (4 bi + bj) bytes, its rows 16 bytes each; blocks
+//         above the diagonal of 16 x 16 blocks are not written
+//   vec : eight fp32 values per token, array after array
+constexpr int kRecT = 0, kRecP = 2048, kRecVec = 4096, kRecBytes = 5120;
+enum {
+  kVecEgk = 0,   // e^g r_k             g: running sum of log a in the chunk, r: 1 / length of the row
+  kVecEq = 1,    // s e^g r_q
+  kVecEk = 2,    // e^(g_last - g) r_k
+  kVecBeta = 3,  // step b
+  kVecG = 4, kVecRk = 5, kVecRq = 6,
+  kVecDlog = 7   // d log a / d gate entry
+};
+constexpr int kRecChain = kRecVec + 4 * 128 + 128;   // what the chains read of it: up to and with kVecG
+
+struct DeltaArgs {
+  int B, T, N, Nq, Nk, K, V;
+  int gate_kind, step_kind, qk_norm;
+  float eps, scale;
+  int state_bf16;              // element type of h0, hT, d_hT, dh0
+  const void *q, *k, *v, *gate, *step, *h0;
+  const float *alpha, *beta;
+  void *y, *hT;
+  char *rec;                   // [slots][N] records; fp32: unused
+  char *states;                // [slots][N] states at a chunk's start (bf16: blocks; fp32: floats), or null
+  char *upd;                   // [slots][N] updates U of a chunk (blocks), or null
+  // backward
+  const void *dy, *d_hT;
+  void *dq, *dk, *dv, *dgate, *dstep, *dh0;
+  char *dstates, *lam;         // like states (at a chunk's end) and upd
+  float *dq_part, *dk_part;    // [TT][shares][K] fp32, or null where a head's are the final ones
+  int shares;                  // CTAs that a token's heads are spread over
+  int32_t *dev_status;
+  long long qs, ks, vs, TT;
+  const int32_t *cu;
+  int nch;                     // chunks of the longest sequence
+  int hpc, wv;                 // chains: heads and 16-column warps per head of a CTA; gradient kernel: heads of a CTA
+};
+
+// First token, length, first chunk slot and chunks of batch entry b.  Of a packed batch, sequence b's slots start at
+// cu[b] / chunk + b: no two overlap, whatever the lengths.  Offsets are cut to 0 .. TT and lengths to T: nothing is
+// addressed beyond what those sized.
+struct DeltaSpan { long long tok0, slot0; int T, n; };
+#ifdef __CUDACC__
+template <int C> __device__ __forceinline__ DeltaSpan delta_span(const DeltaArgs &a, int b) {
+  DeltaSpan s;
+  if (a.cu) {
+    const long long lo = min(max((long long)a.cu[b], 0ll), a.TT), hi = min(max((long long)a.cu[b + 1], lo), a.TT);
+    s.tok0 = lo;
+    s.T = (int)min(hi - lo, (long long)a.T);
+    s.slot0 = lo / C + b;
+  } else {
+    s.tok0 = (long long)b * a.T;
+    s.T = a.T;
+    s.slot0 = (long long)b * a.nch;
+  }
+  s.n = (s.T + C - 1) / C;
+  return s;
+}
+#endif
+inline size_t delta_slots(const m2rnn_delta_params *p, size_t tokens, int C) {
+  return p->cu_seqlens ? tokens / C + p->B : (size_t)p->B * ((p->T + C - 1) / C);
+}
+
+cudaError_t launch_delta_prep(const DeltaArgs &a, cudaStream_t s);        // delta_prep.cu
+cudaError_t launch_delta_chain_fwd(const DeltaArgs &a, cudaStream_t s);   // delta_chain.cu
+cudaError_t launch_delta_chain_bwd(const DeltaArgs &a, cudaStream_t s);
+int delta_grad_heads(const m2rnn_delta_params *p, size_t slots);          // delta_grad.cu: heads of a CTA
+cudaError_t launch_delta_grad(const DeltaArgs &a, cudaStream_t s);
+cudaError_t launch_delta_fwd_f32(const DeltaArgs &a, cudaStream_t s);     // delta_f32.cu
+cudaError_t launch_delta_bwd_f32(const DeltaArgs &a, cudaStream_t s);
+
+struct DeltaStepArgs {
+  int B, N, Nq, Nk, K, V;
+  int gate_kind, step_kind, qk_norm;
+  float eps, scale;
+  const void *q, *k, *v, *gate, *step;
+  const float *alpha, *beta;
+  void *state, *y;
+  const int32_t *slots;
+  int nslots;
+  int32_t *dev_status;
+};
+cudaError_t launch_delta_step(const DeltaStepArgs &a, int io_dtype, int state_dtype, cudaStream_t s);   // delta_decode.cu
+
+struct StateCopyArgs {
+  const char *src;
+  char *dst;
+  const int32_t *src_slots, *dst_slots;
+  int n, src_rows, dst_rows, layers;
+  long long row_bytes, src_layer, dst_layer;   // bytes
+  int32_t *dev_status;
+};
+cudaError_t launch_state_copy(const StateCopyArgs &a, cudaStream_t s);   // state_copy.cu
+int state_copy_limit();
+
+}  // namespace m2rnn

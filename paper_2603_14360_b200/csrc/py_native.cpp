@@ -14,6 +14,7 @@
 #include <ATen/cuda/EmptyTensor.h>
 #include <ATen/ops/zeros.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -555,6 +556,246 @@ PyObject *py_conv_silu_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- gated delta rule and state copy
+
+// The call runs on its tensors' device, whichever is current, and on that device's stream.
+void *stream_on(PyObject *o, const at::Device &dev) {
+  return o == Py_None ? static_cast<void *>(c10::cuda::getCurrentCUDAStream(dev.index()).stream()) : stream_of(o);
+}
+void same_device(const at::Device &dev, std::initializer_list<const Tensor *> ts) {
+  for (const Tensor *t : ts)
+    if (t && t->defined() && t->device() != dev) fail(PyExc_ValueError, "all tensors must be on one device: %s and %s", dev.str().c_str(), t->device().str().c_str());
+}
+void need_cuda(const Tensor &t, const char *name) {
+  if (!t.is_cuda()) fail(PyExc_ValueError, "%s must be a CUDA tensor", name);
+}
+int32_t state_code(const Tensor &t, const char *name) {
+  if (t.scalar_type() == ScalarType::Float) return M2RNN_F32;
+  if (t.scalar_type() == ScalarType::BFloat16) return M2RNN_BF16;
+  fail(PyExc_TypeError, "%s: unsupported state dtype %s", name, c10::toString(t.scalar_type()));
+}
+ScalarType state_type(int32_t code) { return code == M2RNN_BF16 ? ScalarType::BFloat16 : ScalarType::Float; }
+
+// the options that every call of the delta rule takes: gate_kind, alpha, beta, step_kind, qk_norm, norm_eps, q_scale
+struct DeltaOptions { const Tensor *alpha, *beta; };
+DeltaOptions delta_options(m2rnn_delta_params &p, PyObject *const *a) {
+  p.gate_kind = (int32_t)integer(a[0]);
+  p.step_kind = (int32_t)integer(a[3]);
+  p.qk_norm = truth(a[4]);
+  p.norm_eps = (float)real(a[5]);
+  p.q_scale = (float)real(a[6]);
+  return {opt_tensor(a[1], "alpha"), opt_tensor(a[2], "beta")};
+}
+
+struct Delta {
+  Scan s;      // layouts of q, k, v
+  m2rnn_delta_params p{};
+  DeltaOptions o;
+};
+// (q, k, v, gate, step) and the options; states: the first given tensor of these decides the states' type, else `fallback`
+Delta delta_call(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &gate, const Tensor &step, PyObject *const *options, const Tensor *cu,
+                 PyObject *max_seqlen, std::initializer_list<const Tensor *> states, int32_t fallback) {
+  need_cuda(q, "q");
+  Delta d;
+  d.s = scan_params(q, k, v, M2RNN_GATE_LOGIT, 0, 0.0, cu, max_seqlen);
+  const m2rnn_params &f = d.s.p;
+  m2rnn_delta_params &p = d.p;
+  p.B = f.B; p.T = f.T; p.N = f.N; p.Nq = f.Nq; p.Nk = f.Nk; p.K = f.K; p.V = f.V;
+  p.io_dtype = f.io_dtype;
+  p.q_stride = f.q_stride; p.k_stride = f.k_stride; p.v_stride = f.v_stride;
+  p.total_tokens = f.total_tokens; p.cu_seqlens = f.cu_seqlens;
+  d.o = delta_options(p, options);
+  check(q, "q", d.s.tok(p.Nq, p.K), d.s.io, true);
+  check(k, "k", d.s.tok(p.Nk, p.K), d.s.io, true);
+  check(v, "v", d.s.tok(p.N, p.V), d.s.io, true);
+  check(gate, "gate", d.s.gate(), d.s.io);
+  check(step, "step", d.s.gate(), d.s.io);
+  check(d.o.alpha, "alpha", {p.N}, ScalarType::Float);
+  check(d.o.beta, "beta", {p.N}, ScalarType::Float);
+  p.state_dtype = fallback;
+  for (const Tensor *t : states)
+    if (t) { p.state_dtype = state_code(*t, "state"); break; }
+  same_device(q.device(), {&k, &v, &gate, &step, d.o.alpha, d.o.beta, cu});
+  return d;
+}
+
+// delta_fwd(q, k, v, gate, step, h0, [gate_kind, alpha, beta, step_kind, qk_norm, norm_eps, q_scale], save_ckpt, want_hT, state_bf16,
+//           y, hT, ckpt, workspace, stream, cu_seqlens, max_seqlen) -> (y, hT, ckpt)
+PyObject *py_delta_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  want_args(n, 23);
+  const Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k"), &v = tensor(a[2], "v"), &gate = tensor(a[3], "gate"), &step = tensor(a[4], "step");
+  const Tensor *h0 = opt_tensor(a[5], "h0"), *hT_given = opt_tensor(a[17], "hT"), *cu = opt_tensor(a[21], "cu_seqlens");
+  const Delta d = delta_call(q, k, v, gate, step, a + 6, cu, a[22], {h0, hT_given}, truth(a[15]) ? M2RNN_BF16 : M2RNN_F32);
+  const m2rnn_delta_params &p = d.p;
+  const at::Device dev = q.device();
+  const c10::cuda::CUDAGuard guard(dev);
+  const ScalarType st = state_type(p.state_dtype);
+  check(h0, "h0", {p.B, p.N, p.K, p.V}, st);
+  const Tensor y = given_or_empty(opt_tensor(a[16], "y"), d.s.tok(p.N, p.V), d.s.io, dev);
+  check(y, "y", d.s.tok(p.N, p.V), d.s.io);
+  Tensor hT, ckpt, ws;
+  if (hT_given) hT = *hT_given;
+  else if (truth(a[14])) hT = empty({p.B, p.N, p.K, p.V}, st, dev);
+  check(hT.defined() ? &hT : nullptr, "hT", {p.B, p.N, p.K, p.V}, st);
+  if (const Tensor *t = opt_tensor(a[18], "ckpt")) {
+    ckpt = *t;
+    need_cuda(ckpt, "ckpt");
+    if (!ckpt.is_contiguous() || ckpt.nbytes() < m2rnn_delta_ckpt_bytes(&p)) fail(PyExc_ValueError, "ckpt: not contiguous, or smaller than m2rnn_delta_ckpt_bytes");
+  } else if (truth(a[13])) {
+    ckpt = empty({(int64_t)m2rnn_delta_ckpt_bytes(&p)}, ScalarType::Byte, dev);
+  }
+  if (const Tensor *t = opt_tensor(a[19], "workspace")) ws = *t;
+  else if (const size_t need = m2rnn_delta_fwd_workspace_bytes(&p, ckpt.defined())) ws = empty({(int64_t)need}, ScalarType::Byte, dev);
+  same_device(dev, {h0, &y, &hT, &ckpt, &ws});
+  void *stream = stream_on(a[20], dev);
+  int32_t *status = status_of(q);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = m2rnn_delta_fwd(&p, ptr(q), ptr(k), ptr(v), ptr(gate), ptr(step), ptr(h0), fptr(d.o.alpha), fptr(d.o.beta), ptr(y), ptr(hT), ptr(ckpt), ptr(ws),
+                       ws.defined() ? ws.nbytes() : 0, status, stream);
+  Py_END_ALLOW_THREADS
+  check_rc(rc, "m2rnn_delta_fwd");
+  PyObject *r = PyTuple_New(3);
+  if (!r) throw python_error();
+  PyTuple_SET_ITEM(r, 0, back(a[16], y));
+  PyTuple_SET_ITEM(r, 1, back(a[17], hT));
+  PyTuple_SET_ITEM(r, 2, back(a[18], ckpt));
+  return r;
+  END_HANDLE_TH_ERRORS
+}
+
+// delta_bwd(q, k, v, gate, step, h0, [options], dy, d_hT, ckpt, want_dh0, state_bf16, workspace, dq, dk, dv, dgate, dstep, dh0, stream,
+//           cu_seqlens, max_seqlen) -> dict
+PyObject *py_delta_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  want_args(n, 28);
+  const Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k"), &v = tensor(a[2], "v"), &gate = tensor(a[3], "gate"), &step = tensor(a[4], "step");
+  const Tensor *h0 = opt_tensor(a[5], "h0"), &dy = tensor(a[13], "dy"), *d_hT = opt_tensor(a[14], "d_hT"), *ckpt = opt_tensor(a[15], "ckpt");
+  const Tensor *dh0_given = opt_tensor(a[24], "dh0"), *cu = opt_tensor(a[26], "cu_seqlens");
+  const Delta d = delta_call(q, k, v, gate, step, a + 6, cu, a[27], {h0, d_hT, dh0_given}, truth(a[17]) ? M2RNN_BF16 : M2RNN_F32);
+  const m2rnn_delta_params &p = d.p;
+  const at::Device dev = q.device();
+  const c10::cuda::CUDAGuard guard(dev);
+  const ScalarType st = state_type(p.state_dtype), io = d.s.io;
+  check(h0, "h0", {p.B, p.N, p.K, p.V}, st);
+  check(d_hT, "d_hT", {p.B, p.N, p.K, p.V}, st);
+  check(dy, "dy", d.s.tok(p.N, p.V), io);
+  if (ckpt) {
+    need_cuda(*ckpt, "ckpt");
+    if (!ckpt->is_contiguous() || ckpt->nbytes() < m2rnn_delta_ckpt_bytes(&p)) fail(PyExc_ValueError, "ckpt: not contiguous, or smaller than m2rnn_delta_ckpt_bytes");
+  }
+  const Tensor dq = given_or_empty(opt_tensor(a[19], "dq"), q.sizes(), io, dev);
+  const Tensor dk = given_or_empty(opt_tensor(a[20], "dk"), k.sizes(), io, dev);
+  const Tensor dv = given_or_empty(opt_tensor(a[21], "dv"), v.sizes(), io, dev);
+  const Tensor dgate = given_or_empty(opt_tensor(a[22], "dgate"), gate.sizes(), io, dev);
+  const Tensor dstep = given_or_empty(opt_tensor(a[23], "dstep"), step.sizes(), io, dev);
+  Tensor dh0, ws;
+  if (dh0_given) dh0 = *dh0_given;
+  else if (truth(a[16])) dh0 = empty({p.B, p.N, p.K, p.V}, st, dev);
+  check(dq, "dq", q.sizes(), io);
+  check(dk, "dk", k.sizes(), io);
+  check(dv, "dv", v.sizes(), io);
+  check(dgate, "dgate", gate.sizes(), io);
+  check(dstep, "dstep", step.sizes(), io);
+  check(dh0.defined() ? &dh0 : nullptr, "dh0", {p.B, p.N, p.K, p.V}, st);
+  if (const Tensor *t = opt_tensor(a[18], "workspace")) ws = *t;
+  else if (const size_t need = m2rnn_delta_bwd_workspace_bytes(&p, ckpt != nullptr)) ws = empty({(int64_t)need}, ScalarType::Byte, dev);
+  same_device(dev, {h0, &dy, d_hT, ckpt, &dq, &dk, &dv, &dgate, &dstep, &dh0, &ws});
+  void *stream = stream_on(a[25], dev);
+  int32_t *status = status_of(q);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = m2rnn_delta_bwd(&p, ptr(q), ptr(k), ptr(v), ptr(gate), ptr(step), ptr(h0), fptr(d.o.alpha), fptr(d.o.beta), ptr(ckpt), ptr(dy), ptr(d_hT), ptr(dq),
+                       ptr(dk), ptr(dv), ptr(dgate), ptr(dstep), ptr(dh0), ptr(ws), ws.defined() ? ws.nbytes() : 0, status, stream);
+  Py_END_ALLOW_THREADS
+  check_rc(rc, "m2rnn_delta_bwd");
+  return dict_of({{"dq", a[19], &dq}, {"dk", a[20], &dk}, {"dv", a[21], &dv}, {"dgate", a[22], &dgate}, {"dstep", a[23], &dstep}, {"dh0", a[24], &dh0}});
+  END_HANDLE_TH_ERRORS
+}
+
+// delta_decode_step(q, k, v, gate, step, state, [options], slots, y, stream) -> y
+PyObject *py_delta_decode_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  want_args(n, 16);
+  const Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k"), &v = tensor(a[2], "v"), &gate = tensor(a[3], "gate"), &step = tensor(a[4], "step");
+  const Tensor &state = tensor(a[5], "state"), *slots = opt_tensor(a[13], "slots");
+  need_dims(q, "q", 3); need_dims(k, "k", 3); need_dims(v, "v", 3); need_dims(state, "state", 4);
+  m2rnn_delta_params p{};
+  p.B = (int32_t)q.size(0); p.T = 1; p.Nq = (int32_t)q.size(1); p.K = (int32_t)q.size(2);
+  p.Nk = (int32_t)k.size(1); p.N = (int32_t)v.size(1); p.V = (int32_t)v.size(2);
+  p.io_dtype = io_code(q);
+  p.state_dtype = state_code(state, "state");
+  const DeltaOptions o = delta_options(p, a + 6);
+  const ScalarType io = q.scalar_type();
+  const int64_t rows = slots ? state.size(0) : p.B;
+  check(q, "q", {p.B, p.Nq, p.K}, io);
+  check(k, "k", {p.B, p.Nk, p.K}, io);
+  check(v, "v", {p.B, p.N, p.V}, io);
+  check(gate, "gate", {p.B, p.N}, io);
+  check(step, "step", {p.B, p.N}, io);
+  check(state, "state", {rows, p.N, p.K, p.V}, state.scalar_type());
+  check(slots, "slots", {p.B}, ScalarType::Int);
+  check(o.alpha, "alpha", {p.N}, ScalarType::Float);
+  check(o.beta, "beta", {p.N}, ScalarType::Float);
+  const at::Device dev = q.device();
+  const c10::cuda::CUDAGuard guard(dev);
+  const Tensor y = given_or_empty(opt_tensor(a[14], "y"), {p.B, p.N, p.V}, io, dev);
+  check(y, "y", {p.B, p.N, p.V}, io);
+  same_device(dev, {&k, &v, &gate, &step, &state, slots, o.alpha, o.beta, &y});
+  void *stream = stream_on(a[15], dev);
+  int32_t *status = status_of(q);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = m2rnn_delta_decode_step(&p, ptr(q), ptr(k), ptr(v), ptr(gate), ptr(step), fptr(o.alpha), fptr(o.beta), ptr(state),
+                               static_cast<const int32_t *>(ptr(slots)), (int32_t)rows, ptr(y), status, stream);
+  Py_END_ALLOW_THREADS
+  check_rc(rc, "m2rnn_delta_decode_step");
+  return back(a[14], y);
+  END_HANDLE_TH_ERRORS
+}
+
+// state_copy(dst, dst_slots, src_slots, src, axis, stream) -> dst
+PyObject *py_state_copy(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  want_args(n, 6);
+  const Tensor &dst = tensor(a[0], "dst"), &to = tensor(a[1], "dst_slots"), &from = tensor(a[2], "src_slots"), *given = opt_tensor(a[3], "src");
+  const Tensor &src = given ? *given : dst;
+  const int64_t axis = integer(a[4]);
+  if (axis < 0 || axis >= dst.dim()) fail(PyExc_ValueError, "axis %lld: dst has %lld axes", (long long)axis, (long long)dst.dim());
+  need_cuda(dst, "dst");
+  need_dims(src, "src", dst.dim());
+  c10::SmallVector<int64_t, 6> shape(dst.sizes().begin(), dst.sizes().end());
+  shape[axis] = src.size(axis);
+  check(src, "src", shape, dst.scalar_type());
+  check(dst, "dst", dst.sizes(), dst.scalar_type());
+  const int64_t pairs = to.numel();
+  check(to, "dst_slots", {pairs}, ScalarType::Int);
+  check(from, "src_slots", {pairs}, ScalarType::Int);
+  int64_t layers = 1, row = (int64_t)dst.element_size();
+  for (int64_t x = 0; x < axis; ++x) layers *= dst.size(x);
+  for (int64_t x = axis + 1; x < dst.dim(); ++x) row *= dst.size(x);
+  if (pairs > m2rnn_state_copy_limit()) fail(PyExc_ValueError, "%lld pairs: at most %d to a call", (long long)pairs, m2rnn_state_copy_limit());
+  if (row % 16) fail(PyExc_ValueError, "a slot's %lld bytes are not a multiple of 16", (long long)row);
+  if (layers > INT32_MAX || dst.size(axis) > INT32_MAX || src.size(axis) > INT32_MAX) fail(PyExc_ValueError, "too many layers or slots");
+  const at::Device dev = dst.device();
+  same_device(dev, {&src, &to, &from});
+  const char *d0 = static_cast<const char *>(ptr(dst)), *s0 = static_cast<const char *>(ptr(src));
+  if ((d0 != s0 || src.size(axis) != dst.size(axis)) && d0 < s0 + src.nbytes() && s0 < d0 + dst.nbytes()) fail(PyExc_ValueError, "src and dst overlap without being the same");
+  const c10::cuda::CUDAGuard guard(dev);
+  void *stream = stream_on(a[5], dev);
+  int32_t *status = status_of(dst);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = m2rnn_state_copy(ptr(dst), static_cast<const int32_t *>(ptr(to)), (int32_t)dst.size(axis), dst.size(axis) * row, ptr(src),
+                        static_cast<const int32_t *>(ptr(from)), (int32_t)src.size(axis), src.size(axis) * row, (int32_t)pairs, row, (int32_t)layers, status, stream);
+  Py_END_ALLOW_THREADS
+  check_rc(rc, "m2rnn_state_copy");
+  Py_INCREF(a[0]);
+  return a[0];
+  END_HANDLE_TH_ERRORS
+}
+
 // status_word(device index) -> the device's int32 status tensor
 PyObject *py_status_word(PyObject *, PyObject *idx) {
   HANDLE_TH_ERRORS
@@ -578,6 +819,10 @@ PyMethodDef methods[] = {
     {"gated_norm_bwd", FAST(py_gated_norm_bwd)},
     {"conv_silu_fwd", FAST(py_conv_silu_fwd)},
     {"conv_silu_bwd", FAST(py_conv_silu_bwd)},
+    {"delta_fwd", FAST(py_delta_fwd)},
+    {"delta_bwd", FAST(py_delta_bwd)},
+    {"delta_decode_step", FAST(py_delta_decode_step)},
+    {"state_copy", FAST(py_state_copy)},
     {"status_word", py_status_word, METH_O, nullptr},
     {"set_error_class", py_set_error_class, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},

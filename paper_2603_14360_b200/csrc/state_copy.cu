@@ -1,0 +1,92 @@
+// States moved between the slots of a cache: dst[dst_slots[i]] = src[src_slots[i]] for all i at once (a source of -1
+// stands for zeros), in every layer of the cache.
+//
+// All sources are read before any destination is written, although sources and destinations may be slots of the same
+// pool (a compaction shifts, a permutation swaps): a CTA takes a slab of P x 16 bytes of every row, the same bytes of
+// each, holds the n pieces of it in registers, and writes them after a barrier.  Slabs do not touch one another, so
+// nothing has to be ordered between CTAs and no byte passes through scratch.  P is as large as 64 KB of a CTA allow
+// (16 pieces of 16 bytes a thread), a row's slab at least 32 bytes, a sector: that bounds n.
+// Where a destination comes twice the last pair counts; each CTA finds those once (n^2 / 256 comparisons a thread) and
+// walks several slabs.
+#include "delta.h"
+#include "internal.h"
+
+namespace m2rnn {
+namespace {
+
+constexpr int kThreads = 256, kPer = 16, kMost = kThreads * kPer / 2;
+
+__global__ void __launch_bounds__(kThreads, 2) state_copy_kernel(StateCopyArgs a, int log_p, int slabs) {
+  __shared__ int from[kMost], to[kMost];
+  begin_dependent();
+  const int tid = threadIdx.x, P = 1 << log_p;
+  for (int i = tid; i < a.n; i += kThreads) {
+    int s = a.src_slots[i], d = a.dst_slots[i];
+    if (s >= a.src_rows || d >= a.dst_rows) {       // not a slot: the pair is left out
+      if (blockIdx.x == 0 && a.dev_status) atomicExch(a.dev_status, (int32_t)M2RNN_ERR_SHAPE);
+      d = -1;
+    }
+    from[i] = s;
+    to[i] = d;
+  }
+  __syncthreads();
+  unsigned later = 0;      // of this thread's pairs, those that a later one replaces
+  for (int i = tid, x = 0; i < a.n; i += kThreads, ++x) {
+    const int d = to[i];
+    bool again = false;
+    if (d >= 0)
+      for (int o = i + 1; o < a.n; ++o) again |= to[o] == d;
+    later |= (unsigned)again << x;
+  }
+  __syncthreads();
+  for (int i = tid, x = 0; i < a.n; i += kThreads, ++x)
+    if (later >> x & 1) to[i] = -1;
+  __syncthreads();
+  // few pairs: G slabs at a time
+  const int room = (kThreads * kPer) >> log_p, G = room / a.n;
+  const long long w = (long long)P * 16, per_row = (a.row_bytes + w - 1) / w;
+  for (long long first = (long long)blockIdx.x * G; first < slabs; first += (long long)gridDim.x * G) {
+    float4 x[kPer];
+    // what piece r of this thread is: a pair, and where its slab lies; false: none
+    auto piece = [&](int r, int &i, long long &layer, long long &off) {
+      const int q = (tid + r * kThreads) >> log_p, sub = G > 1 ? q / a.n : 0;
+      i = G > 1 ? q - sub * a.n : q;
+      const long long slab = first + sub;
+      if (sub >= G || i >= a.n || slab >= slabs || to[i] < 0) return false;
+      layer = a.layers > 1 ? slab / per_row : 0;
+      off = (slab - layer * per_row) * w + (tid & (P - 1)) * 16;
+      return off < a.row_bytes;
+    };
+#pragma unroll
+    for (int r = 0; r < kPer; ++r) {
+      int i;
+      long long layer, off;
+      x[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (piece(r, i, layer, off) && from[i] >= 0)
+        asm volatile("ld.global.cg.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x[r].x), "=f"(x[r].y), "=f"(x[r].z), "=f"(x[r].w)
+                     : "l"(a.src + layer * a.src_layer + from[i] * a.row_bytes + off) : "memory");
+    }
+    __syncthreads();      // (all of the slab's sources are in registers)
+#pragma unroll
+    for (int r = 0; r < kPer; ++r) {
+      int i;
+      long long layer, off;
+      if (piece(r, i, layer, off)) *reinterpret_cast<float4 *>(a.dst + layer * a.dst_layer + to[i] * a.row_bytes + off) = x[r];
+    }
+  }
+}
+
+}  // namespace
+
+int state_copy_limit() { return kMost; }
+
+cudaError_t launch_state_copy(const StateCopyArgs &a, cudaStream_t s) {
+  // the widest slab whose n pieces a CTA holds; a row's 16-byte pieces (rounded up) at most
+  int log_p = 1;
+  while (log_p < 8 && ((long long)a.n << (log_p + 1)) <= kThreads * kPer && (16ll << log_p) < a.row_bytes) ++log_p;
+  const long long w = 16ll << log_p, per_row = (a.row_bytes + w - 1) / w, slabs = per_row * a.layers, most = (long long)sm_count() * 2, G = ((kThreads * kPer) >> log_p) / a.n, need = (slabs + G - 1) / G;
+  if (slabs > 0x7fffffffll) return cudaErrorInvalidValue;
+  return launch_early(state_copy_kernel, dim3((unsigned)(need < most ? need : most)), dim3(kThreads), 0, s, a, log_p, (int)slabs);
+}
+
+}  // namespace m2rnn
