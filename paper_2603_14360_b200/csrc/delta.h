@@ -25,6 +25,7 @@ enum {
   kVecG = 4, kVecRk = 5, kVecRq = 6,
   kVecDlog = 7   // d log a / d gate entry
 };
+constexpr int kRecF32Bytes = (3 * 256 + 8 * 16) * 4;   // fp32: T, P, M 16 x 16, then the vectors
 constexpr int kRecChain = kRecVec + 4 * 128 + 128;   // what the chains read of it: up to and with kVecG
 
 struct DeltaArgs {
@@ -35,9 +36,9 @@ struct DeltaArgs {
   const void *q, *k, *v, *gate, *step, *h0;
   const float *alpha, *beta;
   void *y, *hT;
-  char *rec;                   // [slots][N] records; fp32: unused
-  char *states;                // [slots][N] states at a chunk's start (bf16: blocks; fp32: floats), or null
-  char *upd;                   // [slots][N] updates U of a chunk (blocks), or null
+  char *rec;                   // [slots][N] records
+  char *states;                // [slots][N] states at a chunk's start (bf16: blocks; fp32: [V][K] floats), or null
+  char *upd;                   // [slots][N] updates U of a chunk (bf16: blocks; fp32: [chunk][V]), or null
   // backward
   const void *dy, *d_hT;
   void *dq, *dk, *dv, *dgate, *dstep, *dh0;

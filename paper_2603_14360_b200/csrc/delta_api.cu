@@ -44,18 +44,16 @@ int check_params(const m2rnn_delta_params *p, bool step) {
   return M2RNN_OK;
 }
 
-// What a forward call leaves for the backward one.  bf16: records, states at the chunks' starts, updates.  fp32: states.
+// What a forward call leaves for the backward one: records, states at the chunks' starts, updates
 struct Ckpt { size_t rec, states, upd, total; };
 Ckpt ckpt_layout(const m2rnn_delta_params *p) {
   Ckpt c{};
   const size_t units = delta_slots(p, tokens_of(p), chunk_of(p)) * p->N, KV = (size_t)p->K * p->V;
-  if (p->io_dtype == M2RNN_F32) {
-    c.total = align_up(units * KV * sizeof(float));
-    return c;
-  }
-  c.states = align_up(units * kRecBytes);
-  c.upd = c.states + align_up(units * KV * 2);
-  c.total = c.upd + align_up(units * kDeltaChunk * p->V * 2);
+  const bool f32 = p->io_dtype == M2RNN_F32;
+  const size_t e = f32 ? 4 : 2;
+  c.states = align_up(units * (f32 ? kRecF32Bytes : kRecBytes));
+  c.upd = c.states + align_up(units * KV * e);
+  c.total = c.upd + align_up(units * chunk_of(p) * p->V * e);
   return c;
 }
 
@@ -67,9 +65,9 @@ Workspace bwd_layout(const m2rnn_delta_params *p, bool have_ckpt) {
   const bool f32 = p->io_dtype == M2RNN_F32;
   w.hpc = f32 ? 1 : delta_grad_heads(p, slots);
   w.dstates = off;
-  if (!f32) off += align_up(units * p->K * p->V * 2);
+  off += align_up(units * p->K * p->V * (f32 ? 4 : 2));
   w.lam = off;
-  if (!f32) off += align_up(units * kDeltaChunk * p->V * 2);
+  off += align_up(units * chunk_of(p) * p->V * (f32 ? 4 : 2));
   const size_t shares = tokens * (p->N / w.hpc) * p->K * sizeof(float);
   w.dq = off;
   if (p->N / p->Nq > w.hpc) off += align_up(shares);
@@ -99,13 +97,10 @@ bool empty_call(const m2rnn_delta_params *p) { return p->B == 0 || p->T == 0 || 
 // the forward kernels; ckpt: where records (and, with `keep`, states and updates) go
 cudaError_t run_fwd(DeltaArgs a, const m2rnn_delta_params *p, char *ckpt, bool keep, cudaStream_t s) {
   const Ckpt c = ckpt_layout(p);
-  if (p->io_dtype == M2RNN_F32) {
-    a.states = keep ? ckpt : nullptr;
-    return launch_delta_fwd_f32(a, s);
-  }
   a.rec = ckpt + c.rec;
   a.states = keep ? ckpt + c.states : nullptr;
   a.upd = keep ? ckpt + c.upd : nullptr;
+  if (p->io_dtype == M2RNN_F32) return launch_delta_fwd_f32(a, s);
   const cudaError_t e = launch_delta_prep(a, s);
   return e != cudaSuccess ? e : launch_delta_chain_fwd(a, s);
 }
@@ -123,7 +118,7 @@ size_t m2rnn_delta_ckpt_bytes(const m2rnn_delta_params *params) {
 }
 
 size_t m2rnn_delta_fwd_workspace_bytes(const m2rnn_delta_params *params, int have_ckpt) {
-  if (check_params(params, false) != M2RNN_OK || empty_call(params) || have_ckpt || params->io_dtype == M2RNN_F32) return 0;
+  if (check_params(params, false) != M2RNN_OK || empty_call(params) || have_ckpt) return 0;
   return ckpt_layout(params).states;      // the records
 }
 
@@ -187,13 +182,12 @@ int m2rnn_delta_bwd(const m2rnn_delta_params *params, const void *q, const void 
   a.dq_part = params->N / params->Nq > w.hpc ? reinterpret_cast<float *>(ws + w.dq) : nullptr;
   a.dk_part = params->N / params->Nk > w.hpc ? reinterpret_cast<float *>(ws + w.dk) : nullptr;
   cudaError_t e;
+  const Ckpt c = ckpt_layout(params);
+  a.rec = kept + c.rec; a.states = kept + c.states; a.upd = kept + c.upd;
+  a.dstates = ws + w.dstates; a.lam = ws + w.lam;
   if (params->io_dtype == M2RNN_F32) {
-    a.states = kept;
     e = launch_delta_bwd_f32(a, s);
   } else {
-    const Ckpt c = ckpt_layout(params);
-    a.rec = kept + c.rec; a.states = kept + c.states; a.upd = kept + c.upd;
-    a.dstates = ws + w.dstates; a.lam = ws + w.lam;
     e = launch_delta_chain_bwd(a, s);
     if (e == cudaSuccess) e = launch_delta_grad(a, s);
   }

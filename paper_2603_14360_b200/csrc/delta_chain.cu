@@ -8,8 +8,9 @@
 // Columns of S are independent recurrences: a warp owns 16 of them and walks the chunks alone.  Everything it holds is
 // transposed, S^T [16 x K] as accumulators of mma.sync m16n8k16: an accumulator tile has the thread <-> element map of
 // the next product's A operand, so S, X, U (and dS, dU, L) never leave registers.  K, Q, V, dY, T and P come as B
-// operands (V, dY as accumulators and A operands) from a ring of shared-memory stages that one warp fills with untiled bulk copies, a row of K, Q, V a
-// lane, padded to an odd number of 16 bytes so that ldmatrix has no conflicts.
+// operands (V, dY as accumulators and A operands) from a ring of shared-memory stages that one warp fills:
+// a record by one untiled bulk copy, rows by cp.async, padded to an odd number of 16 bytes so that ldmatrix has no
+// conflicts.  (Rows by bulk copies, one a lane, were bound by the copies' number: 3.4 us a chunk of K = V = 64.)
 // Roundings to bf16: the operands S, X, U (dS, dU, L), the factored e^(g_last - g) U and the like, and T and P.  S itself
 // is held and updated in fp32.
 #include "delta_common.cuh"
@@ -54,29 +55,29 @@ __device__ __forceinline__ void chain_fill(const DeltaArgs &a, const ChainWork &
       for (int o = i - stages; o < i; ++o) (void)mbar_wait(full + o % stages, (uint32_t)((o / stages) & 1));   // its copies on their way
       return;
     }
-    const uint32_t base = ring + st * sb, kd = base + lane * pitch_k(K), qd = kd + C * pitch_k(K), vd = base + 2 * C * pitch_k(K) + lane * pv,
-                   rd = base + C * (2 * pitch_k(K) + pv);
-    if (have < C && lane >= have) {   // rows behind the last token are zeros
-      for (int o = 0; o < K / 8; ++o) {
-        sts128(kd + 16 * o, make_float4(0.f, 0.f, 0.f, 0.f));
-        sts128(qd + 16 * o, make_float4(0.f, 0.f, 0.f, 0.f));
-      }
-      for (int o = 0; o < 2 * nw; ++o) sts128(vd + 16 * o, make_float4(0.f, 0.f, 0.f, 0.f));
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the stage's next rows come by bulk copies)
-    }
-    __syncwarp();
+    const uint32_t base = ring + st * sb, vd = base + 2 * C * pitch_k(K), rd = vd + C * pv;
     if (lane == 0) {
-      mbar_expect(full + st, (uint32_t)(have * (4 * K + 32 * nw) + a.hpc * kRecChain));
+      mbar_expect(full + st, (uint32_t)(a.hpc * kRecChain));
       const char *rec = a.rec + ((size_t)(sp.slot0 + ch) * a.N + w.n0) * kRecBytes;
       for (int h = 0; h < a.hpc; ++h) bulk_load(rd + h * kRecChain, rec + (size_t)h * kRecBytes, kRecChain, full + st);
     }
-    __syncwarp();
-    if (lane < have) {
-      const long long t = (long long)ch * C + lane;
-      bulk_load(kd, kp + t * a.ks, 2 * K, full + st);
-      bulk_load(qd, qp + t * a.qs, 2 * K, full + st);
-      bulk_load(vd, vp + t * vs, 32 * nw, full + st);
+    // 16 bytes a lane and copy, neighbouring lanes in a row; rows behind the last token are zeros
+    const long long t0 = (long long)ch * C;
+#pragma unroll 4
+    for (int x = lane; x < C * (K / 8); x += 32) {
+      const int r = x / (K / 8), o = x % (K / 8);
+      const bool ok = r < have;
+      cp16_or_zero(base + r * pitch_k(K) + 16 * o, kp + (t0 + (ok ? r : 0)) * a.ks + 8 * o, ok);
+      cp16_or_zero(base + (C + r) * pitch_k(K) + 16 * o, qp + (t0 + (ok ? r : 0)) * a.qs + 8 * o, ok);
     }
+    const int log_v = 31 - __clz(2 * nw);      // pieces of a row of V: a power of two
+#pragma unroll 4
+    for (int x = lane; x < C << log_v; x += 32) {
+      const int r = x >> log_v, o = x & (2 * nw - 1);
+      const bool ok = r < have;
+      cp16_or_zero(vd + r * pv + 16 * o, vp + (t0 + (ok ? r : 0)) * vs + 8 * o, ok);
+    }
+    cp_arrive(full + st);
   }
 }
 
@@ -201,7 +202,7 @@ __global__ void __launch_bounds__(160) delta_chain_fwd_kernel(DeltaArgs a, int s
   __shared__ uint64_t full[8], empty[8];
   const int nw = a.hpc * a.wv, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < stages; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, nw); }
+    for (int i = 0; i < stages; ++i) { mbar_init(full + i, 33); mbar_init(empty + i, nw); }
     fence_mbar_init();
   }
   begin_dependent();
@@ -304,8 +305,6 @@ __global__ void __launch_bounds__(160) delta_chain_fwd_kernel(DeltaArgs a, int s
       }
       rows_out(yt, vat, vsa + 32 * warp + lane * pv, pv, yg, lane < have);
       yg += y_step;
-      // (the stage's next rows come through the other proxy)
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(empty + st);
@@ -319,7 +318,7 @@ __global__ void __launch_bounds__(160) delta_chain_bwd_kernel(DeltaArgs a, int s
   __shared__ uint64_t full[8], empty[8];
   const int nw = a.hpc * a.wv, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < stages; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, nw); }
+    for (int i = 0; i < stages; ++i) { mbar_init(full + i, 33); mbar_init(empty + i, nw); }
     fence_mbar_init();
   }
   begin_dependent();
@@ -416,7 +415,6 @@ __global__ void __launch_bounds__(160) delta_chain_bwd_kernel(DeltaArgs a, int s
       mul_rows<K>(S, A, ksa, l);
       rows_out(dvt, vat, vsa + 32 * warp + lane * pv, pv, dvg + (size_t)ch * C * a.N * V, lane < have);
     }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
     if (lane == 0) mbar_arrive(empty + st);
   }

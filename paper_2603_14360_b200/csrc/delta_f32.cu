@@ -1,59 +1,51 @@
-// Gated delta rule, fp32 (the accuracy path): everything in fp32 FMA, chunks of 16 tokens (the formulas: delta_chain.cu,
-// delta_grad.cu).  A CTA takes one (b, n) and walks its chunks; a chunk's operands lie in shared memory and every
-// product is a loop of FMAs, a column or an entry a thread.  The forward call keeps a state per chunk for the backward
-// call, which recomputes U from it.
+// Gated delta rule, fp32 (the accuracy path): the formulas of delta_prep.cu, delta_chain.cu and delta_grad.cu in chunks of
+// 16 tokens, everything in fp32 FMA.
+//
+//   prep : a CTA a chunk of one head: M, T = (I + M)^-1 by substitution, P, the tokens' factors.
+//   chain: columns of the state are independent recurrences.  Sixteen lanes have a column, K/16 rows each in registers.  Their
+//          sixteen partial products with the chunk's tokens are added by recursive halving, which leaves token t's sum in
+//          lane t: the products with T and P and with the tokens are then FMAs on shuffled values.  A CTA's warps share the
+//          chunk's rows in shared memory (two stages, cp.async); few columns to a CTA where there are few units.
+//   grad : a CTA a chunk of one head, everything of it in shared memory; four tokens' entries of a feature to a thread.
+// States of chunks are kept column after column, [V][K], so that a column's lanes write contiguous floats.
 #include "delta_common.cuh"
 
 namespace m2rnn {
 namespace {
 
-constexpr int C = kDeltaChunkF32, kThreads = 256;
+constexpr int C = kDeltaChunkF32;
+constexpr int kT = 0, kP = C * C, kM = 2 * C * C, kVec = 3 * C * C, kRec = kRecF32Bytes / 4;      // floats of a record
+static_assert(kVec + 8 * C == kRec && kP == C * C, "");
+enum { kBeta = kVecBeta };
 
-// Shared memory of a chunk (floats).  PK, PV: pitches (odd, so that a column's entries fall into different banks).
-struct Lay {
-  int PK, PV, k, q, v, dy, x, u, l, S, D, A, P, m[4], vec, total;
-  __host__ __device__ Lay(int K, int V, bool backward) {
-    PK = K + 1; PV = V + 1;
-    int o = 0;
-    auto take = [&](int n) { const int at = o; o += (n + 3) / 4 * 4; return at; };
-    k = take(C * PK); q = take(C * PK); v = take(C * PV);
-    u = take(C * PV); S = take(K * PV);
-    A = take(C * (C + 1)); P = take(C * (C + 1));
-    vec = take(16 * C);
-    dy = x = l = D = m[0] = m[1] = m[2] = m[3] = 0;
-    if (backward) {
-      dy = take(C * PV); l = take(C * PV); D = take(K * PV);
-      for (int i = 0; i < 4; ++i) m[i] = take(C * PK);
-      x = take(2 * C * (C + 1));
-    }
-    total = o;
-  }
-};
-enum { EG = 0, EK = 1, BT = 2, GS = 3, RK = 4, RQ = 5, DL = 6, DB = 7, SUM = 8 };   // rows of C in vec; SUM ..: sums of the gradient's rows
+// ---- prep
 
-// Loads a chunk's k^, q^ (divided by their lengths), v; the gates; A_ij = e^(g_i - g_j) k^_i . k^_j (j < i), P_ij likewise with s q^ (j <= i)
-__device__ void load_chunk(const DeltaArgs &a, const Lay &y, float *sm, long long tok, int have, int n) {
-  const int K = a.K, V = a.V, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+__global__ void __launch_bounds__(128) delta_prep_f32_kernel(DeltaArgs a) {
+  extern __shared__ __align__(16) float sm[];
+  begin_dependent();
+  const int K = a.K, PK = K + 4, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const long long bc = blockIdx.x / a.N;
+  const int n = (int)(blockIdx.x % a.N), b = (int)(bc / a.nch), ch = (int)(bc % a.nch);
+  const DeltaSpan sp = delta_span<C>(a, b);
+  if (ch >= sp.n) return;
+  const long long tok = sp.tok0 + ch * C;
+  const int have = min(C, sp.T - ch * C);
+  float *ks = sm, *qs = ks + C * PK, *Ms = qs + C * PK, *vec = Ms + C * (C + 4);
   const float *kg = static_cast<const float *>(a.k) + tok * a.ks + (long long)(n / (a.N / a.Nk)) * K;
   const float *qg = static_cast<const float *>(a.q) + tok * a.qs + (long long)(n / (a.N / a.Nq)) * K;
-  const float *vg = static_cast<const float *>(a.v) + tok * a.vs + (long long)n * V;
-  for (int x = tid; x < C * K; x += kThreads) {
-    const int r = x / K, f = x % K;
-    sm[y.k + r * y.PK + f] = r < have ? kg[r * a.ks + f] : 0.f;
-    sm[y.q + r * y.PK + f] = r < have ? qg[r * a.qs + f] : 0.f;
+  for (int x = tid; x < C * (K / 4); x += 128) {
+    const int r = x / (K / 4), o = 4 * (x % (K / 4));
+    const bool ok = r < have;
+    cp16_or_zero(smem_u32(ks + r * PK + o), kg + (ok ? r * a.ks : 0) + o, ok);
+    cp16_or_zero(smem_u32(qs + r * PK + o), qg + (ok ? r * a.qs : 0) + o, ok);
   }
-  for (int x = tid; x < C * V; x += kThreads) {
-    const int r = x / V, f = x % V;
-    sm[y.v + r * y.PV + f] = r < have ? vg[r * a.vs + f] : 0.f;
-  }
-  float *vec = sm + y.vec;
   if (warp == 0) {
-    float la = 0.f, bt = 0.f, dl = 0.f, db = 0.f;
+    float la = 0.f, bt = 0.f, dl = 0.f, unused;
     if (lane < have) {
       const size_t at = (size_t)(tok + lane) * a.N + n;
       const bool psi = a.gate_kind == M2RNN_GATE_PSI;
       la = delta_log_decay(a.gate_kind, static_cast<const float *>(a.gate)[at], psi ? a.alpha[n] : 1.f, psi ? a.beta[n] : 0.f, dl);
-      bt = delta_step_of(a.step_kind, static_cast<const float *>(a.step)[at], db);
+      bt = delta_step_of(a.step_kind, static_cast<const float *>(a.step)[at], unused);
     }
     float gs = la;
 #pragma unroll
@@ -61,72 +53,65 @@ __device__ void load_chunk(const DeltaArgs &a, const Lay &y, float *sm, long lon
       const float o = __shfl_up_sync(0xffffffffu, gs, d);
       if (lane >= d) gs += o;
     }
-    const float last = __shfl_sync(0xffffffffu, gs, C - 1);
     if (lane < C) {
-      vec[C * EG + lane] = expf(gs);
-      vec[C * EK + lane] = expf(last - gs);
-      vec[C * BT + lane] = bt;
-      vec[C * GS + lane] = gs;
-      vec[C * DL + lane] = dl;
-      vec[C * DB + lane] = db;
-      vec[C * RK + lane] = vec[C * RQ + lane] = 1.f;
+      vec[C * kVecG + lane] = gs;
+      vec[C * kBeta + lane] = bt;
+      vec[C * kVecDlog + lane] = dl;
     }
+  }
+  cp_wait_all();
+  __syncthreads();
+  for (int r = warp; r < 2 * C; r += 4) {      // reciprocal lengths
+    const float *row = sm + r * PK;
+    float s = 0.f;
+    for (int f = lane; f < K; f += 32) s = fmaf(row[f], row[f], s);
+#pragma unroll
+    for (int d = 16; d; d /= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
+    if (lane == 0) vec[C * (r < C ? kVecRk : kVecRq) + r % C] = a.qk_norm ? 1.f / sqrtf(s + a.eps) : 1.f;
   }
   __syncthreads();
-  if (a.qk_norm) {      // a warp a row
-    for (int r = warp; r < 2 * C; r += kThreads / 32) {
-      float *row = sm + (r < C ? y.k + r * y.PK : y.q + (r - C) * y.PK);
-      float s = 0.f;
-      for (int f = lane; f < K; f += 32) s = fmaf(row[f], row[f], s);
-#pragma unroll
-      for (int d = 16; d; d /= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
-      const float ri = 1.f / sqrtf(s + a.eps);
-      for (int f = lane; f < K; f += 32) row[f] *= ri;
-      if (lane == 0) vec[C * (r < C ? RK : RQ) + r % C] = ri;
-    }
-    __syncthreads();
+  float *rec = reinterpret_cast<float *>(a.rec) + ((size_t)(sp.slot0 + ch) * a.N + n) * kRec;
+  if (tid < C) {
+    const float gs = vec[C * kVecG + tid], eg = expf(gs), rk = vec[C * kVecRk + tid], rq = vec[C * kVecRq + tid];
+    vec[C * kVecEgk + tid] = eg * rk;
+    vec[C * kVecEq + tid] = a.scale * eg * rq;
+    vec[C * kVecEk + tid] = expf(vec[C * kVecG + C - 1] - gs) * rk;
   }
-  for (int x = tid; x < 2 * C * C; x += kThreads) {
+  for (int x = tid; x < 2 * C * C; x += 128) {
     const int i = x / C % C, j = x % C;
     const bool p = x >= C * C;
     float s = 0.f;
     if (p ? j <= i : j < i) {
-      const float *r = sm + (p ? y.q : y.k) + i * y.PK, *o = sm + y.k + j * y.PK;
-      for (int f = 0; f < K; ++f) s = fmaf(r[f], o[f], s);
-      s *= expf(vec[C * GS + i] - vec[C * GS + j]) * (p ? a.scale : 1.f);
+      const float4 *r = reinterpret_cast<const float4 *>((p ? qs : ks) + i * PK), *o = reinterpret_cast<const float4 *>(ks + j * PK);
+      float s0 = 0.f, s1 = 0.f;
+      for (int f = 0; f < K / 4; ++f) {
+        const float4 u = r[f], w = o[f];
+        s0 = fmaf(u.x, w.x, fmaf(u.y, w.y, s0));
+        s1 = fmaf(u.z, w.z, fmaf(u.w, w.w, s1));
+      }
+      s = (s0 + s1) * expf(vec[C * kVecG + i] - vec[C * kVecG + j]) * vec[C * kVecRk + j] *
+          (p ? a.scale * vec[C * kVecRq + i] : vec[C * kBeta + i] * vec[C * kVecRk + i]);
     }
-    sm[(p ? y.P : y.A) + i * (C + 1) + j] = s;
+    rec[(p ? kP : kM) + i * C + j] = s;
+    if (!p) Ms[i * (C + 4) + j] = s;
   }
   __syncthreads();
-}
-
-// U: a group of 256 / V threads has a column; k^ S first, then the 16 rows one after the other
-__device__ void solve(const Lay &y, float *sm, int K, int V) {
-  const float *vec = sm + y.vec;
-  for (int x = threadIdx.x; x < C * V; x += kThreads) {
-    const int i = x / V, v = x % V;
-    float s0 = 0.f, s1 = 0.f;
-    for (int f = 0; f < K; f += 2) {
-      s0 = fmaf(sm[y.k + i * y.PK + f], sm[y.S + f * y.PV + v], s0);
-      s1 = fmaf(sm[y.k + i * y.PK + f + 1], sm[y.S + (f + 1) * y.PV + v], s1);
-    }
-    sm[y.u + i * y.PV + v] = fmaf(-vec[C * EG + i], s0 + s1, sm[y.v + i * y.PV + v]);
-  }
-  __syncthreads();
-  for (int v = threadIdx.x; v < V; v += kThreads) {
-    float u[C];
+  if (tid < C) {      // column tid of T
+    float t[C];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      float s = sm[y.u + i * y.PV + v];
+      float s = i == tid ? 1.f : 0.f;
 #pragma unroll
-      for (int j = 0; j < i; ++j) s = fmaf(-sm[y.A + i * (C + 1) + j], u[j], s);
-      u[i] = vec[C * BT + i] * s;
+      for (int m = 0; m < i; ++m) s = fmaf(-Ms[i * (C + 4) + m], t[m], s);
+      t[i] = s;
     }
 #pragma unroll
-    for (int i = 0; i < C; ++i) sm[y.u + i * y.PV + v] = u[i];
+    for (int i = 0; i < C; ++i) rec[kT + i * C + tid] = t[i];
   }
-  __syncthreads();
+  rec[kVec + tid] = vec[tid];
 }
+
+// ---- chains
 
 __device__ __forceinline__ float load_state(const void *p, size_t x, int bf16) {
   return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[x]) : static_cast<const float *>(p)[x];
@@ -136,221 +121,402 @@ __device__ __forceinline__ void store_state(void *p, size_t x, int bf16, float v
   else static_cast<float *>(p)[x] = v;
 }
 
-__global__ void __launch_bounds__(kThreads) delta_fwd_f32_kernel(DeltaArgs a) {
-  extern __shared__ __align__(16) float sm[];
-  begin_dependent();
-  const int K = a.K, V = a.V, tid = threadIdx.x, b = blockIdx.x / a.N, n = blockIdx.x % a.N;
-  const Lay y(K, V, false);
-  const DeltaSpan sp = delta_span<C>(a, b);
-  const size_t at = ((size_t)b * a.N + n) * K * V;
-  const float *vec = sm + y.vec;
-  for (int x = tid; x < K * V; x += kThreads) sm[y.S + x / V * y.PV + x % V] = a.h0 ? load_state(a.h0, at + x, a.state_bf16) : 0.f;
-  __syncthreads();
-  for (int ch = 0; ch < sp.n; ++ch) {
-    const long long tok = sp.tok0 + ch * C;
-    const int have = min(C, sp.T - ch * C);
-    if (a.states) {
-      float *o = reinterpret_cast<float *>(a.states) + ((size_t)(sp.slot0 + ch) * a.N + n) * K * V;
-      for (int x = tid; x < K * V; x += kThreads) o[x] = sm[y.S + x / V * y.PV + x % V];
-    }
-    load_chunk(a, y, sm, tok, have, n);
-    solve(y, sm, K, V);
-    if (a.y)
-      for (int x = tid; x < have * V; x += kThreads) {
-        const int i = x / V, v = x % V;
-        float s = 0.f, p = 0.f;
-        for (int f = 0; f < K; ++f) s = fmaf(sm[y.q + i * y.PK + f], sm[y.S + f * y.PV + v], s);
-        for (int j = 0; j <= i; ++j) p = fmaf(sm[y.P + i * (C + 1) + j], sm[y.u + j * y.PV + v], p);
-        static_cast<float *>(a.y)[((size_t)(tok + i) * a.N + n) * V + v] = fmaf(a.scale * vec[C * EG + i], s, p);
-      }
-    __syncthreads();
-    const float ec = vec[C * EG + C - 1];
-    for (int x = tid; x < K * V; x += kThreads) {
-      const int f = x / V, v = x % V;
-      float s = ec * sm[y.S + f * y.PV + v];
+// M adjacent floats
+template <int M> __device__ __forceinline__ void rows_of(const float *p, float (&x)[M]) {
+  if constexpr (M % 4 == 0) {
 #pragma unroll
-      for (int j = 0; j < C; ++j) s = fmaf(vec[C * EK + j] * sm[y.k + j * y.PK + f], sm[y.u + j * y.PV + v], s);
-      sm[y.S + f * y.PV + v] = s;
-    }
-    __syncthreads();
+    for (int i = 0; i < M; i += 4) { const float4 v = *reinterpret_cast<const float4 *>(p + i); x[i] = v.x; x[i + 1] = v.y; x[i + 2] = v.z; x[i + 3] = v.w; }
+  } else if constexpr (M % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < M; i += 2) { const float2 v = *reinterpret_cast<const float2 *>(p + i); x[i] = v.x; x[i + 1] = v.y; }
+  } else {
+#pragma unroll
+    for (int i = 0; i < M; ++i) x[i] = p[i];
   }
-  if (a.hT)
-    for (int x = tid; x < K * V; x += kThreads) store_state(a.hT, at + x, a.state_bf16, sm[y.S + x / V * y.PV + x % V]);
+}
+template <int M> __device__ __forceinline__ void rows_to(float *p, const float (&x)[M]) {
+  if constexpr (M % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < M; i += 4) *reinterpret_cast<float4 *>(p + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+  } else if constexpr (M % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < M; i += 2) *reinterpret_cast<float2 *>(p + i) = make_float2(x[i], x[i + 1]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < M; ++i) p[i] = x[i];
+  }
+}
+// Sums of p[t] over the sixteen lanes of a column; lane t keeps p[t]'s
+__device__ __forceinline__ float halve(float (&p)[C], int l) {
+#pragma unroll
+  for (int h = 8; h; h /= 2) {
+    const bool up = l & h;
+#pragma unroll
+    for (int i = 0; i < h; ++i) {
+      const float send = up ? p[i] : p[h + i], keep = up ? p[h + i] : p[i];
+      p[i] = keep + __shfl_xor_sync(0xffffffffu, send, h);
+    }
+  }
+  return p[0];
+}
+// token t's product rows . S of this lane's column
+template <int M> __device__ __forceinline__ float dots(const float *rows, int pitch, const float (&S)[M], int l) {
+  float p[C];
+#pragma unroll
+  for (int t = 0; t < C; ++t) {
+    float x[M];
+    rows_of<M>(rows + t * pitch + M * l, x);
+    p[t] = 0.f;
+#pragma unroll
+    for (int m = 0; m < M; ++m) p[t] = fmaf(x[m], S[m], p[t]);
+  }
+  return halve(p, l);
 }
 
-__global__ void __launch_bounds__(kThreads) delta_bwd_f32_kernel(DeltaArgs a) {
+constexpr int kStages = 2, kPM = 20;      // pitch of T and P in shared memory: rows as float4 and columns without conflicts
+// Shared memory of a stage (floats): k, q rows, T, P, vectors, nc columns of v (dy)
+constexpr int kSP = C * kPM, kSVec = 2 * C * kPM, kSRec = kSVec + 8 * C;
+__host__ __device__ constexpr int f32_stage(int K, int nc) { return 2 * C * K + kSRec + C * nc; }
+
+// Chunk `ch` on its way into stage `st`; nc (columns of the CTA) a power of two, 16 threads to a column
+template <int K>
+__device__ __forceinline__ void f32_fill(const DeltaArgs &a, const DeltaSpan &sp, int n, int col0, int log_nc, int ch, float *st, const float *kg, const float *qg,
+                                         const float *vg, long long vs) {
+  const int tid = threadIdx.x, nt = 16 << log_nc;
+  const long long tok = (long long)ch * C;
+  const int have = min(C, sp.T - ch * C);
+  for (int x = tid; x < C * (K / 4); x += nt) {
+    const int r = x / (K / 4), o = 4 * (x % (K / 4));
+    const bool ok = r < have;
+    cp16_or_zero(smem_u32(st + r * K + o), kg + (tok + (ok ? r : 0)) * a.ks + o, ok);
+    cp16_or_zero(smem_u32(st + (C + r) * K + o), qg + (tok + (ok ? r : 0)) * a.qs + o, ok);
+  }
+  const float *rec = reinterpret_cast<const float *>(a.rec) + ((size_t)(sp.slot0 + ch) * a.N + n) * kRec;
+  float *sr = st + 2 * C * K;
+  for (int x = tid; x < 2 * C * C / 4; x += nt) cp16(smem_u32(sr + (x >> 2) * kPM + 4 * (x & 3)), rec + 4 * x);      // (T, then P)
+  for (int x = tid; x < 2 * C; x += nt) cp16(smem_u32(sr + kSVec + 4 * x), rec + kVec + 4 * x);
+  const int lp = log_nc - 2;
+  for (int x = tid; x < C << lp; x += nt) {
+    const int r = x >> lp, o = 4 * (x & ((1 << lp) - 1));
+    const bool ok = r < have;
+    cp16_or_zero(smem_u32(sr + kSRec + (r << log_nc) + o), vg + (tok + (ok ? r : 0)) * vs + o, ok);
+  }
+}
+#define F32_COMMIT() asm volatile("cp.async.commit_group;" ::: "memory")
+
+template <int M, bool BWD>
+__global__ void __launch_bounds__(256) delta_chain_f32_kernel(DeltaArgs a) {
   extern __shared__ __align__(16) float sm[];
   begin_dependent();
-  const int K = a.K, V = a.V, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, b = blockIdx.x / a.N, n = blockIdx.x % a.N;
-  const Lay y(K, V, true);
+  constexpr int K = 16 * M;
+  const int nc = blockDim.x / 16, V = a.V, slabs = V / nc, lane = threadIdx.x & 31, l = lane & 15, base = lane & 16;
+  const int unit = blockIdx.x / slabs, b = unit / a.N, n = unit % a.N, col0 = blockIdx.x % slabs * nc, mine = threadIdx.x / 16, v = col0 + mine;
   const DeltaSpan sp = delta_span<C>(a, b);
-  const size_t at = ((size_t)b * a.N + n) * K * V;
-  float *vec = sm + y.vec;
-  for (int x = tid; x < K * V; x += kThreads) sm[y.D + x / V * y.PV + x % V] = a.d_hT ? load_state(a.d_hT, at + x, a.state_bf16) : 0.f;
-  __syncthreads();
-  for (int ch = sp.n - 1; ch >= 0; --ch) {
+  const size_t at = ((size_t)b * a.N + n) * K * V + v;
+  const void *in = BWD ? a.d_hT : a.h0;
+  void *out = BWD ? a.dh0 : a.hT;
+  float S[M];      // rows M l ..
+#pragma unroll
+  for (int m = 0; m < M; ++m) S[m] = in ? load_state(in, at + (size_t)(M * l + m) * V, a.state_bf16) : 0.f;
+  const long long vs = BWD ? (long long)a.N * V : a.vs;
+  const float *vg = static_cast<const float *>(BWD ? a.dy : a.v) + sp.tok0 * vs + (long long)n * V + col0;
+  const float *kg = static_cast<const float *>(a.k) + sp.tok0 * a.ks + (long long)(n / (a.N / a.Nk)) * K;
+  const float *qg = static_cast<const float *>(a.q) + sp.tok0 * a.qs + (long long)(n / (a.N / a.Nq)) * K;
+  const int stage = f32_stage(K, nc), log_nc = 31 - __clz(nc);
+  if (sp.n > 0) f32_fill<K>(a, sp, n, col0, log_nc, BWD ? sp.n - 1 : 0, sm, kg, qg, vg, vs);
+  F32_COMMIT();
+  for (int i = 0; i < sp.n; ++i) {
+    const int ch = BWD ? sp.n - 1 - i : i, have = min(C, sp.T - ch * C);
+    if (i + 1 < sp.n) f32_fill<K>(a, sp, n, col0, log_nc, BWD ? ch - 1 : ch + 1, sm + ((i + 1) & 1) * stage, kg, qg, vg, vs);
+    F32_COMMIT();
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    __syncthreads();
+    const float *ks = sm + (i & 1) * stage, *qs = ks + C * K, *rec = qs + C * K, *vec = rec + kSVec, *vt = rec + kSRec;
     const long long tok = sp.tok0 + ch * C;
-    const int have = min(C, sp.T - ch * C);
-    const float *sg = reinterpret_cast<const float *>(a.states) + ((size_t)(sp.slot0 + ch) * a.N + n) * K * V;
-    for (int x = tid; x < K * V; x += kThreads) sm[y.S + x / V * y.PV + x % V] = sg[x];
-    for (int x = tid; x < C * V; x += kThreads) {
-      const int r = x / V, v = x % V;
-      sm[y.dy + r * y.PV + v] = r < have ? static_cast<const float *>(a.dy)[((size_t)(tok + r) * a.N + n) * V + v] : 0.f;
-    }
-    load_chunk(a, y, sm, tok, have, n);
-    solve(y, sm, K, V);
-    // dU, then L = (I + b A)^-T dU from the last row up
-    for (int x = tid; x < C * V; x += kThreads) {
-      const int j = x / V, v = x % V;
-      float s = 0.f, p = 0.f;
-      for (int f = 0; f < K; ++f) s = fmaf(sm[y.k + j * y.PK + f], sm[y.D + f * y.PV + v], s);
-      for (int i = j; i < C; ++i) p = fmaf(sm[y.P + i * (C + 1) + j], sm[y.dy + i * y.PV + v], p);
-      sm[y.l + j * y.PV + v] = fmaf(vec[C * EK + j], s, p);
-    }
-    __syncthreads();
-    for (int v = tid; v < V; v += kThreads) {
-      float l[C];      // b L below: what row j takes of the rows behind it
+    const size_t slot = (size_t)(sp.slot0 + ch) * a.N + n;
+    const float x0 = vt[l * nc + mine], ec = expf(vec[C * kVecG + C - 1]);
+    float *states = reinterpret_cast<float *>(BWD ? a.dstates : a.states);
+    if (states) rows_to<M>(states + slot * K * V + (size_t)v * K + M * l, S);
+    if constexpr (!BWD) {
+      float T[C], P[C];      // this lane's token's rows
+      rows_of<C>(rec + l * kPM, T);
+      rows_of<C>(rec + kSP + l * kPM, P);
+      const float x = vec[C * kBeta + l] * fmaf(-vec[C * kVecEgk + l], dots<M>(ks, K, S, l), x0);
+      float u = 0.f;
 #pragma unroll
-      for (int j = C - 1; j >= 0; --j) {
-        float s = sm[y.l + j * y.PV + v];
+      for (int j = 0; j < C; ++j) u = fmaf(T[j], __shfl_sync(0xffffffffu, x, base + j), u);      // (T_lj = 0 for j > l)
+      float y = 0.f;
+      if (a.y) y = vec[C * kVecEq + l] * dots<M>(qs, K, S, l);
 #pragma unroll
-        for (int i = j + 1; i < C; ++i) s = fmaf(-sm[y.A + i * (C + 1) + j], l[i], s);
-        sm[y.l + j * y.PV + v] = s;
-        l[j] = vec[C * BT + j] * s;
-      }
-    }
-    __syncthreads();
-    for (int x = tid; x < have * V; x += kThreads) {
-      const int i = x / V, v = x % V;
-      static_cast<float *>(a.dv)[((size_t)(tok + i) * a.N + n) * V + v] = vec[C * BT + i] * sm[y.l + i * y.PV + v];
-    }
-    // E dP (s in it) and E N
-    for (int x = tid; x < 2 * C * C; x += kThreads) {
-      const int i = x / C % C, j = x % C;
-      const bool p = x < C * C;
-      float s = 0.f;
-      if (p ? j <= i : j < i) {
-        const float *r = sm + (p ? y.dy : y.l) + i * y.PV, *u = sm + y.u + j * y.PV;
-        for (int v = 0; v < V; ++v) s = fmaf(r[v], u[v], s);
-        s *= expf(vec[C * GS + i] - vec[C * GS + j]) * (p ? a.scale : -1.f);
-      }
-      sm[y.x + (p ? 0 : C * (C + 1)) + i * (C + 1) + j] = s;
-    }
-    __syncthreads();
-    // dQ^, dK-, dK+
-    for (int x = tid; x < C * K; x += kThreads) {
-      const int i = x / K, f = x % K;
-      float ys = 0.f, ls = 0.f, us = 0.f;
-      for (int v = 0; v < V; ++v) {
-        const float S = sm[y.S + f * y.PV + v];
-        ys = fmaf(sm[y.dy + i * y.PV + v], S, ys);
-        ls = fmaf(sm[y.l + i * y.PV + v], S, ls);
-        us = fmaf(sm[y.u + i * y.PV + v], sm[y.D + f * y.PV + v], us);
-      }
-      ys *= a.scale * vec[C * EG + i];
-      ls *= -vec[C * EG + i];
-      us *= vec[C * EK + i];
-      const float first = us;
-      for (int j = 0; j <= i; ++j) {
-        ys = fmaf(sm[y.x + i * (C + 1) + j], sm[y.k + j * y.PK + f], ys);
-        ls = fmaf(sm[y.x + C * (C + 1) + i * (C + 1) + j], sm[y.k + j * y.PK + f], ls);
-      }
-      for (int j = i; j < C; ++j) {
-        us = fmaf(sm[y.x + j * (C + 1) + i], sm[y.q + j * y.PK + f], us);
-        us = fmaf(vec[C * BT + j] * sm[y.x + C * (C + 1) + j * (C + 1) + i], sm[y.k + j * y.PK + f], us);
-      }
-      sm[y.m[0] + i * y.PK + f] = ys;
-      sm[y.m[1] + i * y.PK + f] = ls;
-      sm[y.m[2] + i * y.PK + f] = us;
-      sm[y.m[3] + i * y.PK + f] = first;
-    }
-    float ss = 0.f;      // <S, dS'>
-    for (int x = tid; x < K * V; x += kThreads) ss = fmaf(sm[y.S + x / V * y.PV + x % V], sm[y.D + x / V * y.PV + x % V], ss);
-    __syncthreads();
-    // sums of a row: q^ . dQ^, k^ . dK-, k^ . dK+, k^ . (e^(g_last - g) dS' U), L . v
-    for (int i = warp; i < C; i += kThreads / 32) {
-      float d[5] = {};
-      for (int f = lane; f < K; f += 32) {
-        const float q = sm[y.q + i * y.PK + f], k = sm[y.k + i * y.PK + f];
-        d[0] = fmaf(q, sm[y.m[0] + i * y.PK + f], d[0]);
-#pragma unroll
-        for (int m = 1; m < 4; ++m) d[m] = fmaf(k, sm[y.m[m] + i * y.PK + f], d[m]);
-      }
-      for (int v = lane; v < V; v += 32) d[4] = fmaf(sm[y.l + i * y.PV + v], sm[y.v + i * y.PV + v], d[4]);
-#pragma unroll
-      for (int m = 0; m < 5; ++m) {
-#pragma unroll
-        for (int o = 16; o; o /= 2) d[m] += __shfl_xor_sync(0xffffffffu, d[m], o);
-        if (lane == 0) vec[C * (SUM + m) + i] = d[m];
-      }
-    }
-#pragma unroll
-    for (int o = 16; o; o /= 2) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    if (lane == 0) vec[C * (SUM + 5) + warp] = ss;
-    __syncthreads();
-    const float ec = vec[C * EG + C - 1];
-    if (warp == 0) {
-      const int i = lane & (C - 1);
-      float part = lane < C ? vec[C * SUM + i] + vec[C * BT + i] * vec[C * (SUM + 1) + i] - vec[C * (SUM + 2) + i] : 0.f, all = lane < C ? vec[C * (SUM + 3) + i] : 0.f;
-      float sd = lane < kThreads / 32 ? vec[C * (SUM + 5) + lane] : 0.f;
-#pragma unroll
-      for (int o = 16; o; o /= 2) {
-        all += __shfl_xor_sync(0xffffffffu, all, o);
-        sd += __shfl_xor_sync(0xffffffffu, sd, o);
-      }
-#pragma unroll
-      for (int o = 1; o < C; o *= 2) {
-        const float t = __shfl_down_sync(0xffffffffu, part, o);
-        if (lane + o < C) part += t;
-      }
-      if (lane < have) {
-        const size_t x = (size_t)(tok + lane) * a.N + n;
-        static_cast<float *>(a.dgate)[x] = (part + all + ec * sd) * vec[C * DL + lane];
-        static_cast<float *>(a.dstep)[x] = (vec[C * (SUM + 4) + lane] + vec[C * (SUM + 1) + lane]) * vec[C * DB + lane];
-      }
-    }
-    // dq, dk through the division by the lengths
-    for (int x = tid; x < have * K; x += kThreads) {
-      const int i = x / K, f = x % K;
-      const float bt = vec[C * BT + i];
-      float dq = sm[y.m[0] + i * y.PK + f], dk = fmaf(bt, sm[y.m[1] + i * y.PK + f], sm[y.m[2] + i * y.PK + f]);
-      if (a.qk_norm) {
-        dq = vec[C * RQ + i] * fmaf(-sm[y.q + i * y.PK + f], vec[C * SUM + i], dq);
-        dk = vec[C * RK + i] * fmaf(-sm[y.k + i * y.PK + f], fmaf(bt, vec[C * (SUM + 1) + i], vec[C * (SUM + 2) + i]), dk);
-      }
-      const size_t t = (size_t)(tok + i);
-      if (a.dq_part) a.dq_part[(t * a.N + n) * K + f] = dq;
-      else static_cast<float *>(a.dq)[(t * a.N + n) * K + f] = dq;
-      if (a.dk_part) a.dk_part[(t * a.N + n) * K + f] = dk;
-      else static_cast<float *>(a.dk)[(t * a.N + n) * K + f] = dk;
-    }
-    // dS
-    for (int x = tid; x < K * V; x += kThreads) {
-      const int f = x / V, v = x % V;
-      float s = ec * sm[y.D + f * y.PV + v];
+      for (int m = 0; m < M; ++m) S[m] *= ec;
 #pragma unroll
       for (int j = 0; j < C; ++j) {
-        s = fmaf(a.scale * vec[C * EG + j] * sm[y.q + j * y.PK + f], sm[y.dy + j * y.PV + v], s);
-        s = fmaf(-vec[C * EG + j] * vec[C * BT + j] * sm[y.k + j * y.PK + f], sm[y.l + j * y.PV + v], s);
+        const float uj = __shfl_sync(0xffffffffu, u, base + j), e = uj * vec[C * kVecEk + j];
+        y = fmaf(P[j], uj, y);
+        float k[M];
+        rows_of<M>(ks + j * K + M * l, k);
+#pragma unroll
+        for (int m = 0; m < M; ++m) S[m] = fmaf(k[m], e, S[m]);
       }
-      sm[y.D + f * y.PV + v] = s;
+      if (a.y && l < have) static_cast<float *>(a.y)[((size_t)(tok + l) * a.N + n) * V + v] = y;
+      if (a.upd) reinterpret_cast<float *>(a.upd)[slot * C * V + l * V + v] = u;
+    } else {
+      // x0: dY
+      float du = vec[C * kVecEk + l] * dots<M>(ks, K, S, l);
+#pragma unroll
+      for (int i2 = 0; i2 < C; ++i2) du = fmaf(rec[kSP + i2 * kPM + l], __shfl_sync(0xffffffffu, x0, base + i2), du);      // (P_il = 0 for i < l)
+      float L = 0.f;
+#pragma unroll
+      for (int i2 = 0; i2 < C; ++i2) L = fmaf(rec[i2 * kPM + l], __shfl_sync(0xffffffffu, du, base + i2), L);
+      const float dv = vec[C * kBeta + l] * L;
+      if (l < have) static_cast<float *>(a.dv)[((size_t)(tok + l) * a.N + n) * V + v] = dv;
+      reinterpret_cast<float *>(a.lam)[slot * C * V + l * V + v] = L;
+      const float e = vec[C * kVecEq + l] * x0, f = -vec[C * kVecEgk + l] * dv;
+#pragma unroll
+      for (int m = 0; m < M; ++m) S[m] *= ec;
+#pragma unroll
+      for (int j = 0; j < C; ++j) {
+        const float ej = __shfl_sync(0xffffffffu, e, base + j), fj = __shfl_sync(0xffffffffu, f, base + j);
+        float k[M], q[M];
+        rows_of<M>(ks + j * K + M * l, k);
+        rows_of<M>(qs + j * K + M * l, q);
+#pragma unroll
+        for (int m = 0; m < M; ++m) S[m] = fmaf(q[m], ej, fmaf(k[m], fj, S[m]));
+      }
     }
-    __syncthreads();
+    __syncthreads();      // (the stage is the next but one's)
   }
-  if (a.dh0)
-    for (int x = tid; x < K * V; x += kThreads) store_state(a.dh0, at + x, a.state_bf16, sm[y.D + x / V * y.PV + x % V]);
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  if (out)
+#pragma unroll
+    for (int m = 0; m < M; ++m) store_state(out, at + (size_t)(M * l + m) * V, a.state_bf16, S[m]);
 }
 
-cudaError_t launch(void (*kernel)(DeltaArgs), const DeltaArgs &a, bool backward, cudaStream_t s) {
-  const size_t smem = (size_t)Lay(a.K, a.V, backward).total * sizeof(float);
-  const cudaError_t e = allow_smem(kernel, smem);
+// ---- grad
+
+constexpr int kThreads = 256;
+// Shared memory (floats): S, dS' [V][K]; dY, L, U [V][kPM]; k, q [C][K + 1]; five arrays [C][K + 1]; four matrices; the vectors; sums
+__host__ __device__ constexpr int grad_floats(int K, int V) { return 2 * K * V + 3 * V * kPM + 7 * C * (K + 1) + 4 * C * C + 8 * C + 8 * C + 16; }
+static_assert(grad_floats(128, 128) * 4 <= 227 * 1024, "");
+
+__global__ void __launch_bounds__(kThreads) delta_grad_f32_kernel(DeltaArgs a) {
+  extern __shared__ __align__(16) float sm[];
+  begin_dependent();
+  const int K = a.K, V = a.V, PK = K + 1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const long long bc = blockIdx.x / a.N;
+  const int n = (int)(blockIdx.x % a.N), b = (int)(bc / a.nch), ch = (int)(bc % a.nch);
+  const DeltaSpan sp = delta_span<C>(a, b);
+  if (ch >= sp.n) return;
+  const long long tok = sp.tok0 + ch * C;
+  const int have = min(C, sp.T - ch * C);
+  const size_t slot = (size_t)(sp.slot0 + ch) * a.N + n;
+  float *S = sm, *D = S + K * V, *yt = D + K * V, *lt = yt + V * kPM, *ut = lt + V * kPM;
+  float *XP = ut + V * kPM, *XPt = XP + C * C, *XN = XPt + C * C, *XNt = XN + C * C, *vec = XNt + C * C, *sums = vec + 8 * C;
+  float *ks = sums + 8 * C + 16, *qs = ks + C * PK, *m0 = qs + C * PK;      // five arrays from m0: dQ^, dK-, dK+, and R's and W's parts
+  const float *rec = reinterpret_cast<const float *>(a.rec) + slot * kRec;
+  {
+    const float *sg = reinterpret_cast<const float *>(a.states) + slot * K * V, *dg = reinterpret_cast<const float *>(a.dstates) + slot * K * V;
+    for (int x = tid; x < K * V / 4; x += kThreads) {
+      cp16(smem_u32(S + 4 * x), sg + 4 * x);
+      cp16(smem_u32(D + 4 * x), dg + 4 * x);
+    }
+    if (tid < 2 * C) cp16(smem_u32(vec + 4 * tid), rec + kVec + 4 * tid);
+    const float *yg = static_cast<const float *>(a.dy) + ((size_t)tok * a.N + n) * V;
+    const float *ug = reinterpret_cast<const float *>(a.upd) + slot * C * V, *lg = reinterpret_cast<const float *>(a.lam) + slot * C * V;
+    const int log_v = 31 - __clz(V);
+    for (int x = tid; x < C * V; x += kThreads) {
+      const int r = x >> log_v, v = x & (V - 1);
+      yt[v * kPM + r] = r < have ? yg[(size_t)r * a.N * V + v] : 0.f;
+      ut[v * kPM + r] = ug[x];
+      lt[v * kPM + r] = lg[x];
+    }
+    const float *kg = static_cast<const float *>(a.k) + tok * a.ks + (long long)(n / (a.N / a.Nk)) * K;
+    const float *qg = static_cast<const float *>(a.q) + tok * a.qs + (long long)(n / (a.N / a.Nq)) * K;
+    for (int x = tid; x < C * K; x += kThreads) {
+      const int r = x / K, f = x % K;
+      ks[r * PK + f] = r < have ? kg[r * a.ks + f] : 0.f;
+      qs[r * PK + f] = r < have ? qg[r * a.qs + f] : 0.f;
+    }
+    cp_wait_all();
+  }
+  __syncthreads();
+  float ss = 0.f;      // <S, dS'>
+  for (int x = tid; x < K * V; x += kThreads) ss = fmaf(S[x], D[x], ss);
+#pragma unroll
+  for (int o = 16; o; o /= 2) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+  if (lane == 0) sums[8 * C + warp] = ss;
+  // dP, N: one entry a thread; G
+  {
+    const int i = tid / C, j = tid % C;
+    float p = 0.f, m = 0.f, gg = 0.f, xp = 0.f, xn = 0.f;
+    if (j <= i) {
+      for (int v = 0; v < V; ++v) {
+        p = fmaf(yt[v * kPM + i], ut[v * kPM + j], p);
+        m = fmaf(-lt[v * kPM + i], ut[v * kPM + j], m);
+      }
+      const float e = expf(vec[C * kVecG + i] - vec[C * kVecG + j]);
+      xp = a.scale * e * p;
+      if (j < i) {
+        xn = e * m;
+        gg = fmaf(rec[kP + i * C + j], p, rec[kM + i * C + j] * m);
+      }
+    }
+    XP[i * C + j] = XPt[j * C + i] = xp;
+    XN[i * C + j] = XNt[j * C + i] = xn;
+    // sums of G's rows (a half warp has one), and of its columns through shared memory
+    float r = gg;
+#pragma unroll
+    for (int o = 8; o; o /= 2) r += __shfl_xor_sync(0xffffffffu, r, o);
+    if (j == 0) sums[5 * C + i] = r;
+    m0[i * PK + j] = gg;
+  }
+  __syncthreads();
+  if (tid < C) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < C; ++i) s += m0[i * PK + tid];
+    sums[6 * C + tid] = s;
+  }
+  __syncthreads();
+  const int AR = C * PK;      // one of the five arrays
+  for (int x = tid; x < 4 * K; x += kThreads) {
+    const int f = x % K, i0 = 4 * (x / K);
+    float y[4] = {}, ls[4] = {}, us[4] = {};
+    for (int v = 0; v < V; ++v) {
+      const float s = S[v * K + f], d = D[v * K + f];
+      const float4 y4 = *reinterpret_cast<const float4 *>(yt + v * kPM + i0), l4 = *reinterpret_cast<const float4 *>(lt + v * kPM + i0), u4 = *reinterpret_cast<const float4 *>(ut + v * kPM + i0);
+      const float yy[4] = {y4.x, y4.y, y4.z, y4.w}, ll[4] = {l4.x, l4.y, l4.z, l4.w}, uu[4] = {u4.x, u4.y, u4.z, u4.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        y[e] = fmaf(yy[e], s, y[e]);
+        ls[e] = fmaf(ll[e], s, ls[e]);
+        us[e] = fmaf(uu[e], d, us[e]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = i0 + e;
+      const float g = vec[C * kVecG + i], eg = expf(g), rk = vec[C * kVecRk + i], rq = vec[C * kVecRq + i];
+      y[e] *= a.scale * eg;
+      ls[e] *= -eg;
+      us[e] *= expf(vec[C * kVecG + C - 1] - g);
+      m0[3 * AR + i * PK + f] = fmaf(rq * qs[i * PK + f], y[e], vec[C * kBeta + i] * rk * ks[i * PK + f] * ls[e]);
+      m0[4 * AR + i * PK + f] = rk * ks[i * PK + f] * us[e];
+    }
+    for (int j = 0; j < C; ++j) {
+      const float kj = ks[j * PK + f], kr = vec[C * kVecRk + j] * kj, kb = vec[C * kBeta + j] * kr, qr = vec[C * kVecRq + j] * qs[j * PK + f];
+      const float4 a4 = *reinterpret_cast<const float4 *>(XPt + j * C + i0), b4 = *reinterpret_cast<const float4 *>(XNt + j * C + i0);
+      const float4 c4 = *reinterpret_cast<const float4 *>(XP + j * C + i0), d4 = *reinterpret_cast<const float4 *>(XN + j * C + i0);
+      const float aa[4] = {a4.x, a4.y, a4.z, a4.w}, bb[4] = {b4.x, b4.y, b4.z, b4.w}, cc[4] = {c4.x, c4.y, c4.z, c4.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        y[e] = fmaf(aa[e], kr, y[e]);
+        ls[e] = fmaf(bb[e], kr, ls[e]);
+        us[e] = fmaf(cc[e], qr, fmaf(dd[e], kb, us[e]));
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      m0[(i0 + e) * PK + f] = y[e];
+      m0[AR + (i0 + e) * PK + f] = ls[e];
+      m0[2 * AR + (i0 + e) * PK + f] = us[e];
+    }
+  }
+  __syncthreads();
+  for (int i = warp; i < C; i += kThreads / 32) {      // q^ . dQ^, k^ . dK-, k^ . dK+, R, W, L . v
+    float d[6] = {};
+    for (int f = lane; f < K; f += 32) {
+      const float q = vec[C * kVecRq + i] * qs[i * PK + f], k = vec[C * kVecRk + i] * ks[i * PK + f];
+      d[0] = fmaf(q, m0[i * PK + f], d[0]);
+      d[1] = fmaf(k, m0[AR + i * PK + f], d[1]);
+      d[2] = fmaf(k, m0[2 * AR + i * PK + f], d[2]);
+      d[3] += m0[3 * AR + i * PK + f];
+      d[4] += m0[4 * AR + i * PK + f];
+    }
+    if (i < have) {
+      const float *vg = static_cast<const float *>(a.v) + (tok + i) * a.vs + (long long)n * V;
+      for (int v = lane; v < V; v += 32) d[5] = fmaf(lt[v * kPM + i], vg[v], d[5]);
+    }
+#pragma unroll
+    for (int m = 0; m < 6; ++m) {
+#pragma unroll
+      for (int o = 16; o; o /= 2) d[m] += __shfl_xor_sync(0xffffffffu, d[m], o);
+      if (lane == 0) sums[C * (m < 5 ? m : 7) + i] = d[m];
+    }
+  }
+  __syncthreads();
+  if (warp == 0) {
+    const int i = lane & (C - 1);
+    const float w = sums[4 * C + i];
+    float all = lane < C ? w : 0.f, part = lane < C ? sums[3 * C + i] + sums[5 * C + i] - w - sums[6 * C + i] : 0.f, sd = lane < kThreads / 32 ? sums[8 * C + lane] : 0.f;
+#pragma unroll
+    for (int o = 16; o; o /= 2) {
+      all += __shfl_xor_sync(0xffffffffu, all, o);
+      sd += __shfl_xor_sync(0xffffffffu, sd, o);
+    }
+#pragma unroll
+    for (int o = 1; o < C; o *= 2) {
+      const float t = __shfl_down_sync(0xffffffffu, part, o);
+      if (lane + o < C) part += t;
+    }
+    if (lane < have) {
+      const size_t x = (size_t)(tok + lane) * a.N + n;
+      float db;
+      (void)delta_step_of(a.step_kind, static_cast<const float *>(a.step)[x], db);
+      static_cast<float *>(a.dgate)[x] = (part + all + expf(vec[C * kVecG + C - 1]) * sd) * vec[C * kVecDlog + lane];
+      static_cast<float *>(a.dstep)[x] = (sums[7 * C + lane] + sums[C + lane]) * db;
+    }
+  }
+  // dq, dk through the division by the lengths
+  for (int x = tid; x < have * K; x += kThreads) {
+    const int i = x / K, f = x % K;
+    const float bt = vec[C * kBeta + i], rk = vec[C * kVecRk + i], rq = vec[C * kVecRq + i];
+    float dq = m0[i * PK + f], dk = fmaf(bt, m0[AR + i * PK + f], m0[2 * AR + i * PK + f]);
+    if (a.qk_norm) {
+      dq = rq * fmaf(-rq * qs[i * PK + f], sums[i], dq);
+      dk = rk * fmaf(-rk * ks[i * PK + f], fmaf(bt, sums[C + i], sums[2 * C + i]), dk);
+    }
+    const size_t t = (size_t)(tok + i);
+    (a.dq_part ? a.dq_part : static_cast<float *>(a.dq))[(t * a.N + n) * K + f] = dq;      // (N shares, or N heads)
+    (a.dk_part ? a.dk_part : static_cast<float *>(a.dk))[(t * a.N + n) * K + f] = dk;
+  }
+}
+
+template <int M, bool BWD> cudaError_t chain_m(const DeltaArgs &a, cudaStream_t s) {
+  // columns of a CTA: sixteen, fewer where that leaves SMs without one
+  const long long units = (long long)a.B * a.N;
+  int nc = 16;
+  while (nc > 4 && units * (a.V / nc) < sm_count()) nc /= 2;
+  const size_t smem = (size_t)kStages * f32_stage(a.K, nc) * sizeof(float);
+  const cudaError_t e = allow_smem(delta_chain_f32_kernel<M, BWD>, smem);
   if (e != cudaSuccess) return e;
-  return launch_early(kernel, dim3((unsigned)((long long)a.B * a.N)), dim3(kThreads), smem, s, a);
+  return launch_early(delta_chain_f32_kernel<M, BWD>, dim3((unsigned)(units * (a.V / nc))), dim3(16 * nc), smem, s, a);
+}
+template <bool BWD> cudaError_t chain(const DeltaArgs &a, cudaStream_t s) {
+  switch (a.K) {
+    case 16: return chain_m<1, BWD>(a, s);
+    case 32: return chain_m<2, BWD>(a, s);
+    case 48: return chain_m<3, BWD>(a, s);
+    case 64: return chain_m<4, BWD>(a, s);
+    case 80: return chain_m<5, BWD>(a, s);
+    case 96: return chain_m<6, BWD>(a, s);
+    case 112: return chain_m<7, BWD>(a, s);
+    default: return chain_m<8, BWD>(a, s);
+  }
 }
 
 }  // namespace
 
-cudaError_t launch_delta_fwd_f32(const DeltaArgs &a, cudaStream_t s) { return launch(delta_fwd_f32_kernel, a, false, s); }
-cudaError_t launch_delta_bwd_f32(const DeltaArgs &a, cudaStream_t s) { return launch(delta_bwd_f32_kernel, a, true, s); }
+cudaError_t launch_delta_fwd_f32(const DeltaArgs &a, cudaStream_t s) {
+  const size_t smem = (size_t)(2 * C * (a.K + 4) + C * (C + 4) + 8 * C) * sizeof(float);
+  const cudaError_t e = launch_early(delta_prep_f32_kernel, dim3((unsigned)((long long)a.B * a.nch * a.N)), dim3(128), smem, s, a);
+  return e != cudaSuccess ? e : chain<false>(a, s);
+}
+cudaError_t launch_delta_bwd_f32(const DeltaArgs &a, cudaStream_t s) {
+  cudaError_t e = chain<true>(a, s);
+  const size_t smem = (size_t)grad_floats(a.K, a.V) * sizeof(float);
+  if (e == cudaSuccess) e = allow_smem(delta_grad_f32_kernel, smem);
+  return e != cudaSuccess ? e : launch_early(delta_grad_f32_kernel, dim3((unsigned)((long long)a.B * a.nch * a.N)), dim3(kThreads), smem, s, a);
+}
 
 }  // namespace m2rnn

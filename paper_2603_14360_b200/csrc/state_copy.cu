@@ -19,7 +19,7 @@ constexpr int kThreads = 256, kPer = 16, kMost = kThreads * kPer / 2;
 __global__ void __launch_bounds__(kThreads, 2) state_copy_kernel(StateCopyArgs a, int log_p, int slabs) {
   __shared__ int from[kMost], to[kMost];
   begin_dependent();
-  const int tid = threadIdx.x, P = 1 << log_p;
+  const int tid = threadIdx.x, P = 1 << log_p;      // pieces of a slab
   for (int i = tid; i < a.n; i += kThreads) {
     int s = a.src_slots[i], d = a.dst_slots[i];
     if (s >= a.src_rows || d >= a.dst_rows) {       // not a slot: the pair is left out
@@ -42,36 +42,26 @@ __global__ void __launch_bounds__(kThreads, 2) state_copy_kernel(StateCopyArgs a
   for (int i = tid, x = 0; i < a.n; i += kThreads, ++x)
     if (later >> x & 1) to[i] = -1;
   __syncthreads();
-  // few pairs: G slabs at a time
-  const int room = (kThreads * kPer) >> log_p, G = room / a.n;
-  const long long w = (long long)P * 16, per_row = (a.row_bytes + w - 1) / w;
-  for (long long first = (long long)blockIdx.x * G; first < slabs; first += (long long)gridDim.x * G) {
+  const unsigned per_row = (unsigned)((a.row_bytes + 16ll * P - 1) / (16ll * P));
+  for (unsigned slab = blockIdx.x; slab < (unsigned)slabs; slab += gridDim.x) {
+    const unsigned layer = a.layers > 1 ? slab / per_row : 0;
+    const long long first = (long long)(slab - layer * per_row) * 16 * P;
+    const char *src = a.src + layer * a.src_layer + first;
+    char *dst = a.dst + layer * a.dst_layer + first;
     float4 x[kPer];
-    // what piece r of this thread is: a pair, and where its slab lies; false: none
-    auto piece = [&](int r, int &i, long long &layer, long long &off) {
-      const int q = (tid + r * kThreads) >> log_p, sub = G > 1 ? q / a.n : 0;
-      i = G > 1 ? q - sub * a.n : q;
-      const long long slab = first + sub;
-      if (sub >= G || i >= a.n || slab >= slabs || to[i] < 0) return false;
-      layer = a.layers > 1 ? slab / per_row : 0;
-      off = (slab - layer * per_row) * w + (tid & (P - 1)) * 16;
-      return off < a.row_bytes;
-    };
 #pragma unroll
     for (int r = 0; r < kPer; ++r) {
-      int i;
-      long long layer, off;
+      const int q = tid + r * kThreads, i = q >> log_p, off = (q & (P - 1)) * 16;
       x[r] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (piece(r, i, layer, off) && from[i] >= 0)
+      if (i < a.n && to[i] >= 0 && from[i] >= 0 && first + off < a.row_bytes)
         asm volatile("ld.global.cg.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x[r].x), "=f"(x[r].y), "=f"(x[r].z), "=f"(x[r].w)
-                     : "l"(a.src + layer * a.src_layer + from[i] * a.row_bytes + off) : "memory");
+                     : "l"(src + from[i] * a.row_bytes + off) : "memory");
     }
     __syncthreads();      // (all of the slab's sources are in registers)
 #pragma unroll
     for (int r = 0; r < kPer; ++r) {
-      int i;
-      long long layer, off;
-      if (piece(r, i, layer, off)) *reinterpret_cast<float4 *>(a.dst + layer * a.dst_layer + to[i] * a.row_bytes + off) = x[r];
+      const int q = tid + r * kThreads, i = q >> log_p, off = (q & (P - 1)) * 16;
+      if (i < a.n && to[i] >= 0 && first + off < a.row_bytes) *reinterpret_cast<float4 *>(dst + to[i] * a.row_bytes + off) = x[r];
     }
   }
 }
@@ -81,12 +71,14 @@ __global__ void __launch_bounds__(kThreads, 2) state_copy_kernel(StateCopyArgs a
 int state_copy_limit() { return kMost; }
 
 cudaError_t launch_state_copy(const StateCopyArgs &a, cudaStream_t s) {
-  // the widest slab whose n pieces a CTA holds; a row's 16-byte pieces (rounded up) at most
+  // the widest slab whose n pieces a CTA holds; no wider than a row, nor (down to 512 bytes) than leaves a slab for each CTA
+  const long long most = (long long)sm_count() * 2;
+  auto slabs_of = [&](int l) { return (a.row_bytes + (16ll << l) - 1) / (16ll << l) * a.layers; };
   int log_p = 1;
-  while (log_p < 8 && ((long long)a.n << (log_p + 1)) <= kThreads * kPer && (16ll << log_p) < a.row_bytes) ++log_p;
-  const long long w = 16ll << log_p, per_row = (a.row_bytes + w - 1) / w, slabs = per_row * a.layers, most = (long long)sm_count() * 2, G = ((kThreads * kPer) >> log_p) / a.n, need = (slabs + G - 1) / G;
+  while (((long long)a.n << (log_p + 1)) <= kThreads * kPer && (16ll << log_p) < a.row_bytes && (log_p < 5 || slabs_of(log_p + 1) >= most)) ++log_p;
+  const long long slabs = slabs_of(log_p);
   if (slabs > 0x7fffffffll) return cudaErrorInvalidValue;
-  return launch_early(state_copy_kernel, dim3((unsigned)(need < most ? need : most)), dim3(kThreads), 0, s, a, log_p, (int)slabs);
+  return launch_early(state_copy_kernel, dim3((unsigned)(slabs < most ? slabs : most)), dim3(kThreads), 0, s, a, log_p, (int)slabs);
 }
 
 }  // namespace m2rnn
