@@ -49,6 +49,7 @@ struct DeltaArgs {
   long long qs, ks, vs, TT;
   const int32_t *cu;
   int nch;                     // chunks of the longest sequence
+  int per_q, per_k;            // heads to a q head, to a k head
   int hpc, wv;                 // chains: heads and 16-column warps per head of a CTA; gradient kernel: heads of a CTA
 };
 

@@ -90,6 +90,7 @@ DeltaArgs base_args(const m2rnn_delta_params *p, const void *q, const void *k, c
   a.TT = (long long)tokens_of(p);
   a.cu = p->cu_seqlens;
   a.nch = (p->T + chunk_of(p) - 1) / chunk_of(p);
+  a.per_q = p->N / p->Nq; a.per_k = p->N / p->Nk;
   return a;
 }
 bool empty_call(const m2rnn_delta_params *p) { return p->B == 0 || p->T == 0 || tokens_of(p) == 0; }

@@ -1,331 +1,348 @@
 // Gated delta rule, bf16: gradients of q, k, the gate and the step, chunk by chunk, from what the chains kept
-// (delta_chain.cu: S at a chunk's start, U; dS' at its end, L = dU through T^T).  With K^, Q^ the rows divided by
-// their lengths, E_ij = e^(g_i - g_j), and dP_ij = dY_i . U_j (j <= i), N_ij = -L_i . U_j (j < i):
-//     dQ^ = s (e^g dY S^T + (E dP) K^)
-//     dK- = -e^g L S^T + (E N) K^                     its step b_i left out: k's part in what the update reads
-//     dK+ = e^(g_last - g) U dS'^T + (b E N)^T K^ + s (E dP)^T Q^        k's part in what it writes
-//     dK^ = b dK- + dK+        db_i = L_i . v_i + k^_i . dK-_i
+// (delta_chain.cu: S at a chunk's start, U; dS' at its end, L = dU through T^T).  With r_q, r_k the reciprocal lengths,
+// E_ij = e^(g_i - g_j), dP_ij = dY_i . U_j and N_ij = -L_i . U_j, two 32 x 32 matrices
+//     X1_ij = s r_q,i r_k,j E_ij dP_ij   (j <= i)        X2_ij = b_i r_k,i r_k,j E_ij N_ij   (j < i)
+// serve both sides of their products:
+//     dq' = s e^g r_q dY S^T + X1 K                                          (r_q times the gradient of q r_q)
+//     dk' = -b e^g r_k L S^T + e^(g_last - g) r_k U dS'^T + (X2 + X2^T) K + X1^T Q
+// Every sum over features that is needed comes from three of the products with the states, a1 = q . dY S^T, a2 = k . L S^T,
+// a3 = k . U dS'^T, and from the rows and columns of X1 (.) Q K^T and X2 (.) K K^T:
+//     dx = x' - r^2 x (x . x')  (the division by the lengths)        db_i = L_i . v_i - e^g r_k a2 + sum_j X2_ij k_i . k_j / b_i
 // The decays' gradient sums what crosses token t's decay: what tokens from t on read of S, what tokens before t write
 // into S', the pairs on either side of it, and S on its way to S':
-//     R_i = q^_i . (s e^g S dY)_i - b_i k^_i . (e^g S L)_i        W_j = k^_j . (e^(g_last - g) dS' U)_j
-//     G_ij = E_ij (s (q^_i . k^_j) dP_ij + b_i (k^_i . k^_j) N_ij)      (j < i)
+//     R_i = s e^g r_q a1 - b e^g r_k a2        W_j = e^(g_last - g) r_k a3        G_ij = X1_ij q_i . k_j + X2_ij k_i . k_j   (j < i)
 //     d log a_t = e^g_last <S, dS'> + sum_{i >= t} R_i + sum_{j < t} W_j + sum_{j < t <= i} G_ij
-// (With q . dQ^ - k . dK+ in place of R, W and G the pairs on one side of t would cancel only up to the roundings of
+// (With q . dq - k . dk in place of R, W and G the pairs on one side of t would cancel only up to the roundings of
 // the matrices to bf16: 2.5e-2 off where states decay within a few tokens.  Here the same fp32 value is added and taken away.)
-// Four warps: 16 tokens x half of the K features each; the products over V in slabs of 64 columns.  A CTA takes a chunk
-// of `hpc` heads that share q and k, one after the other, and adds up their dq and dk in registers.
+//
+// Eight warps: 16 tokens x a quarter of the K features each; the products over V in slabs of 64 columns (32 where K > 64).
+// A job is a chunk of `hpc` heads that share q and k, one after the other, their dq and dk added up in registers.  Two CTAs
+// to an SM walk over the jobs, the next slab (and the next job's rows) on its way while one is worked on: with a CTA a job the
+// loads' latency stood between a third of the cycles.  What the chains wrote is contiguous and comes by untiled bulk
+// copies; rows of q, k, v and dY by cp.async.
 #include "delta_common.cuh"
 
 namespace m2rnn {
 namespace {
 
-constexpr int C = kDeltaChunk;
+constexpr int C = kDeltaChunk, kThreads = 256;
 
 template <int K> struct GradCfg {
   static constexpr int kPK = 2 * K + 16;
-  static constexpr int kQ = 0, kK = C * kPK, kMat = 2 * C * kPK;        // q, k rows; four 32 x 32 matrices as blocks
-  static constexpr int kVec = kMat + 4 * 2048;                           // the record's vectors
-  static constexpr int kRed = kVec + 1024;                               // float [8][32] sums of the two halves; [2][32] each of G's rows and columns; [32] L.v; [4] <S, dS'>
-  static constexpr int kSlab = kRed + (10 * 32 + 4 * 32 + 32 + 16) * 4;        // dY, V rows, then U, L, S, dS' blocks of a slab
+  static constexpr int kRows = 2 * C * kPK, kMat = 2 * kRows;            // q, k rows, twice; X1, X2 as blocks
+  static constexpr int kRed = kMat + 2 * 2048;                           // sums, see Red
+  static constexpr int kSlab = kRed + 27 * 128 + 128;                    // slabs: the vectors, dY, V rows, then U, L, S, dS' blocks
+  static constexpr int NT = (K + 31) / 32;                               // 8-feature tiles of a warp, most
+  static constexpr int VS = K > 64 ? 32 : 64;                            // columns of a slab, most
   static_assert(kSlab % 16 == 0, "");
 };
-__host__ __device__ constexpr int slab_bytes(int K, int VS) { return 2 * C * (2 * VS + 16) + 2 * 2 * C * VS + 2 * 2 * K * VS; }
+// rows of 32 floats: a1, a2, a3 by quarter; sums of X1 (.) QK^T and X2 (.) KK^T / b over a row's entries by quarter; over a
+// column's by half; X1 (.) QK^T's diagonal; L . v; the factors of the division by the lengths; <S, dS'> by warp
+enum Red { kA = 0, kRow1 = 12, kRow2 = 16, kCol = 20, kDiag = 22, kLv = 23, kUq = 24, kUk = 25, kSds = 26 };
+__host__ __device__ constexpr int slab_bytes(int K, int VS) { return 1024 + 2 * C * (2 * VS + 16) + 2 * 2 * C * VS + 2 * 2 * K * VS; }
 
-// MULTI: several heads to a CTA
-template <int K, bool MULTI>
-__global__ void __launch_bounds__(128, 2) delta_grad_kernel(DeltaArgs a) {
+struct GradJob { long long tok; size_t slot; int have, n0, run, hq, hk; };      // have = 0: no more
+
+// MULTI: several heads to a job; VS: columns of a slab
+template <int K, bool MULTI, int VS>
+__global__ void __launch_bounds__(kThreads, 2) delta_grad_kernel(DeltaArgs a, unsigned jobs) {
   using Cfg = GradCfg<K>;
-  constexpr int NT = K / 16;     // 8-feature tiles of a warp
+  constexpr int NT = Cfg::NT;
   extern __shared__ __align__(128) unsigned char smem[];
-  begin_dependent();
+  __shared__ uint64_t full[2];
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = tid & 31, g = lane >> 2, c = lane & 3;
-  const int mh = warp & 1, kh = warp >> 1, i0 = 16 * mh, f0 = kh * (K / 2);
-  const int runs = a.N / a.hpc;
-  const long long bc = blockIdx.x / runs;
-  const int run = (int)(blockIdx.x % runs), n0 = run * a.hpc;
-  const int b = (int)(bc / a.nch), ch = (int)(bc % a.nch);
-  const DeltaSpan sp = delta_span<C>(a, b);
-  if (ch >= sp.n) return;
-  const long long tok = sp.tok0 + ch * C;
-  const int have = min(C, sp.T - ch * C), V = a.V, VS = V < 64 ? V : 64, pv = 2 * VS + 16;
-  const int hq = n0 / (a.N / a.Nq), hk = n0 / (a.N / a.Nk);
-  const uint32_t base = smem_u32(smem), qsa = base + Cfg::kQ, ksa = base + Cfg::kK, mat = base + Cfg::kMat;
-  const uint32_t ysa = base + Cfg::kSlab, vsa = ysa + C * pv, usa = vsa + C * pv, lsa = usa + 2 * C * VS, ssa = lsa + 2 * C * VS, dsa = ssa + 2 * K * VS;
-  const float *vec = reinterpret_cast<const float *>(smem + Cfg::kVec);
-  float *red = reinterpret_cast<float *>(smem + Cfg::kRed), *grow = red + 10 * 32, *gcol = grow + 64, *lv = gcol + 64, *sds = lv + 32;
-  const uint32_t mrow = lane & 7, mlo = (lane >> 3) & 1, mhi = lane >> 4;
-
-  {
-    const __nv_bfloat16 *kg = static_cast<const __nv_bfloat16 *>(a.k) + tok * a.ks + (long long)hk * K;
-    const __nv_bfloat16 *qg = static_cast<const __nv_bfloat16 *>(a.q) + tok * a.qs + (long long)hq * K;
-    for (int x = tid; x < C * (K / 8); x += 128) {
-      const int r = x / (K / 8), o = x % (K / 8);
-      const bool ok = r < have;
-      cp16_or_zero(ksa + r * Cfg::kPK + 16 * o, kg + (ok ? r * a.ks : 0) + 8 * o, ok);
-      cp16_or_zero(qsa + r * Cfg::kPK + 16 * o, qg + (ok ? r * a.qs : 0) + 8 * o, ok);
-    }
+  if (tid == 0) {
+    mbar_init(full, 1);
+    mbar_init(full + 1, 1);
+    fence_mbar_init();
   }
-  const uint32_t qat = qsa + (i0 + g) * Cfg::kPK + 2 * (f0 + 2 * c), kat = ksa + (i0 + g) * Cfg::kPK + 2 * (f0 + 2 * c);   // this thread's entries
-  // results: to their shares, or to the places of q and k
-  auto emit = [&](const float (&oq)[NT][4], const float (&ok)[NT][4]) {
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int i = i0 + g + 8 * x;
-        const size_t at = ((size_t)(tok + i) * a.shares + run) * K + f0 + 8 * t + 2 * c;
-        if (!a.dq_part) sts32(qat + 8 * x * Cfg::kPK + 16 * t, __uint_as_float(pack_bf16(oq[t][2 * x], oq[t][2 * x + 1])));
-        else if (i < have) *reinterpret_cast<float2 *>(a.dq_part + at) = make_float2(oq[t][2 * x], oq[t][2 * x + 1]);
-        if (!a.dk_part) sts32(kat + 8 * x * Cfg::kPK + 16 * t, __uint_as_float(pack_bf16(ok[t][2 * x], ok[t][2 * x + 1])));
-        else if (i < have) *reinterpret_cast<float2 *>(a.dk_part + at) = make_float2(ok[t][2 * x], ok[t][2 * x + 1]);
-      }
+  const int mh = warp & 1, kq = warp >> 1, i0 = 16 * mh, f0 = 8 * NT * kq;      // tokens i0 .., features f0 ..
+  const int tiles = K % 32 == 0 ? NT : min(NT, max(0, K / 8 - NT * kq));        // 8-feature tiles that this warp has
+  const bool low = kq <= 2 * mh + 1;                                            // tile (16 mh, 8 kq) of 32 x 32: not above the diagonal's blocks
+  constexpr int pv = 2 * VS + 16, P = VS / 8, slab = slab_bytes(K, VS), UB = 2 * C * VS, SB = 2 * K * VS;      // P: pieces of a row; bytes of U, of S
+  const int V = a.V, parts = (unsigned)V / VS;
+  const uint32_t base = smem_u32(smem), mat = base + Cfg::kMat;
+  float *red = reinterpret_cast<float *>(smem + Cfg::kRed);
+  const uint32_t mrow = lane & 7, mlo = (lane >> 3) & 1, mhi = lane >> 4;
+  const unsigned runs = (unsigned)(a.N / a.hpc);
+  begin_dependent();
+  __syncthreads();
+
+  // the first job from number j on that there is (of a packed batch's shorter sequences some are not)
+  auto find = [&](unsigned &j) {
+    GradJob o{};
+    for (; j < jobs; j += gridDim.x) {
+      const unsigned bc = j / runs, run = j - bc * runs;
+      const int b = (int)(bc / (unsigned)a.nch), ch = (int)(bc - (unsigned)b * a.nch);
+      const DeltaSpan sp = delta_span<C>(a, b);
+      if (ch >= sp.n) continue;
+      o.tok = sp.tok0 + ch * C;
+      o.slot = (size_t)(sp.slot0 + ch) * a.N;
+      o.have = min(C, sp.T - ch * C);
+      o.run = (int)run;
+      o.n0 = (int)run * a.hpc;
+      o.hq = (int)((unsigned)o.n0 / (unsigned)a.per_q);
+      o.hk = (int)((unsigned)o.n0 / (unsigned)a.per_k);
+      break;
+    }
+    return o;
   };
+  // rows of q and k of a job, and slab `part` of its head n, on their way
+  auto fetch_rows = [&](const GradJob &o, int qb) {
+    const __nv_bfloat16 *kg = static_cast<const __nv_bfloat16 *>(a.k) + o.tok * a.ks + o.hk * K;
+    const __nv_bfloat16 *qg = static_cast<const __nv_bfloat16 *>(a.q) + o.tok * a.qs + o.hq * K;
+    for (int x = tid; x < C * (K / 8); x += kThreads) {
+      const int r = x / (K / 8), p = x % (K / 8);
+      const bool ok = r < o.have;
+      const uint32_t at = base + qb * Cfg::kRows + r * Cfg::kPK + 16 * p;
+      cp16_or_zero(at, qg + (ok ? r * a.qs : 0) + 8 * p, ok);
+      cp16_or_zero(at + C * Cfg::kPK, kg + (ok ? r * a.ks : 0) + 8 * p, ok);
+    }
+  };
+  auto fetch = [&](const GradJob &o, int n, int part, int buf) {
+    const int vb = part * VS;
+    const uint32_t at = base + Cfg::kSlab + buf * slab, ysa = at + 1024, vsa = ysa + C * pv, usa = vsa + C * pv;
+    if (tid == 0) {
+      const size_t slot = o.slot + n, u = slot * (2 * C * V) + 2 * C * vb, x = slot * (2 * K * V) + 2 * K * vb;
+      mbar_expect(full + buf, 1024 + 2 * (UB + SB));
+      bulk_load(at, a.rec + slot * kRecBytes + kRecVec, 1024, full + buf);
+      bulk_load(usa, a.upd + u, UB, full + buf);
+      bulk_load(usa + UB, a.lam + u, UB, full + buf);
+      bulk_load(usa + 2 * UB, a.states + x, SB, full + buf);
+      bulk_load(usa + 2 * UB + SB, a.dstates + x, SB, full + buf);
+    }
+    if (tid < C * P) {      // (one piece a thread: P <= 8)
+      const int r = tid / P, p = tid % P;
+      const bool ok = r < o.have;
+      const long long t = o.tok + (ok ? r : 0), col = (long long)n * V + vb + 8 * p;
+      cp16_or_zero(ysa + r * pv + 16 * p, static_cast<const __nv_bfloat16 *>(a.dy) + t * a.N * V + col, ok);
+      cp16_or_zero(vsa + r * pv + 16 * p, static_cast<const __nv_bfloat16 *>(a.v) + t * a.vs + col, ok);
+    }
+  };
+  unsigned j = blockIdx.x;
+  GradJob o = find(j);
+  if (!o.have) return;
+  fetch_rows(o, 0);
+  fetch(o, o.n0, 0, 0);
+  bool fine = true;
+  unsigned cnt = 0;      // slabs so far: the buffer's parity and its barrier's phase
+  for (int qb = 0;; qb ^= 1) {
+  const uint32_t qsa = base + qb * Cfg::kRows, ksa = qsa + C * Cfg::kPK, qat = qsa + (i0 + g) * Cfg::kPK + 2 * (f0 + 2 * c), kat = qat + C * Cfg::kPK;   // (at: this thread's entries)
+  GradJob next{};
+
+  // results: to their shares, or to the places of q and k
+  auto emit_to = [&](const float (&x)[NT][4], float *part, uint32_t at) {
+    if (part) {
+      part += ((size_t)(o.tok + i0 + g) * a.shares + o.run) * K + f0 + 2 * c;
+#pragma unroll
+      for (int h = 0; h < 2; ++h, part += (size_t)8 * a.shares * K)
+        if (i0 + g + 8 * h < o.have)
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+            if (t < tiles) *reinterpret_cast<float2 *>(part + 8 * t) = make_float2(x[t][2 * h], x[t][2 * h + 1]);
+    } else {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (t < tiles) sts32(at + 8 * h * Cfg::kPK + 16 * t, __uint_as_float(pack_bf16(x[t][2 * h], x[t][2 * h + 1])));
+    }
+  };
+  auto emit = [&](const float (&oq)[NT][4], const float (&ok)[NT][4]) { emit_to(oq, a.dq_part, qat); emit_to(ok, a.dk_part, kat); };
   float dqs[MULTI ? NT : 1][4], dks[MULTI ? NT : 1][4];
   if constexpr (MULTI)
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) dqs[t][r] = dks[t][r] = 0.f;
-
+  float qk[4], kk[4];                         // q k^T and k k^T, tile (16 mh, 8 kq)
+  float dq[NT][4], dm[NT][4], dp[NT][4];      // dY S^T, L S^T, U dS'^T; then dq', dk'
+  float yu[4], lu[4], ld[4];                  // tiles (16 mh, 8 kq): dY U^T, L U^T, L V^T
+  float ss;                                   // this thread's part of <S, dS'>
   for (int h = 0; h < a.hpc; ++h) {
-    const int n = n0 + h;
-    const size_t slot = (size_t)(sp.slot0 + ch) * a.N + n;
-    const char *rec = a.rec + slot * kRecBytes;
-    if (tid < 64) cp16(base + Cfg::kVec + 16 * tid, rec + kRecVec + 16 * tid);
-    float dq[NT][4], dm[NT][4], dp[NT][4];      // dY S^T, L S^T, U dS'^T; then dQ^, dK-, dK+
+    const int n = o.n0 + h;
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int r = 0; r < 4; ++r) {
+      yu[r] = lu[r] = ld[r] = 0.f;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) dq[t][r] = dm[t][r] = dp[t][r] = 0.f;
-    float yu[2][4] = {}, lu[2][4] = {}, ld[2][4] = {};    // tiles (16 mh, 16 kh): dY U^T, L U^T, L V^T
-    float ss = 0.f;                                        // this thread's part of <S, dS'>
-    for (int vb = 0; vb < V; vb += VS) {
-      {
-        const __nv_bfloat16 *yg = static_cast<const __nv_bfloat16 *>(a.dy) + ((size_t)tok * a.N + n) * V + vb;
-        const __nv_bfloat16 *vg = static_cast<const __nv_bfloat16 *>(a.v) + tok * a.vs + (long long)n * V + vb;
-        const long long ys = (long long)a.N * V;
-        const int per = VS / 8;
-        for (int x = tid; x < C * per; x += 128) {
-          const int r = x / per, o = x % per;
-          const bool ok = r < have;
-          cp16_or_zero(ysa + r * pv + 16 * o, yg + (ok ? r * ys : 0) + 8 * o, ok);
-          cp16_or_zero(vsa + r * pv + 16 * o, vg + (ok ? r * a.vs : 0) + 8 * o, ok);
-        }
-        const char *ug = a.upd + slot * (2 * C * V) + 2 * C * vb, *lg = a.lam + slot * (2 * C * V) + 2 * C * vb;
-        for (int x = tid; x < C * VS / 8; x += 128) {
-          cp16(usa + 16 * x, ug + 16 * x);
-          cp16(lsa + 16 * x, lg + 16 * x);
-        }
-        const char *sg = a.states + slot * (2 * K * V) + 2 * K * vb, *dg = a.dstates + slot * (2 * K * V) + 2 * K * vb;
-        for (int x = tid; x < K * VS / 8; x += 128) {
-          cp16(ssa + 16 * x, sg + 16 * x);
-          cp16(dsa + 16 * x, dg + 16 * x);
-        }
-        cp_wait_all();
-        __syncthreads();
+      for (int t = 0; t < NT; ++t) dq[t][r] = dm[t][r] = dp[t][r] = 0.f;
+    }
+    ss = 0.f;
+    const float *vec = nullptr;
+    for (int part = 0; part < parts; ++part, ++cnt) {
+    const int bi = cnt & 1;
+    cp_wait_all();
+    if (fine) {      // (after a wait that ran out the rest is worked through with whatever there is: every access is in bounds)
+      fine = mbar_wait(full + bi, (cnt >> 1) & 1);
+      if (!fine && lane == 0) report_timeout(a.dev_status);
+    }
+    __syncthreads();
+    if (part + 1 < parts) fetch(o, n, part + 1, bi ^ 1);
+    else if (h + 1 < a.hpc) fetch(o, n + 1, 0, bi ^ 1);
+    else {
+      j += gridDim.x;
+      next = find(j);
+      if (next.have) {
+        fetch_rows(next, qb ^ 1);
+        fetch(next, next.n0, 0, bi ^ 1);
       }
-      // <S, dS'>
-      for (int x = tid; x < K * VS / 8; x += 128) {
-        const uint4 p = *reinterpret_cast<const uint4 *>(smem + (ssa - base) + 16 * x), d = *reinterpret_cast<const uint4 *>(smem + (dsa - base) + 16 * x);
+    }
+    unsigned char *buf = smem + Cfg::kSlab + bi * slab;
+    const uint32_t at0 = base + Cfg::kSlab + bi * slab, ysa = at0 + 1024, vsa = ysa + C * pv, usa = vsa + C * pv, ssa = usa + 2 * UB;
+    vec = reinterpret_cast<const float *>(buf);
+    if (h == 0 && part == 0) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) qk[r] = kk[r] = 0.f;
+      if (low) {
+#pragma unroll
+        for (int kt = 0; kt < K / 16; ++kt) {
+          uint32_t qa[4], ka[4], kb[2];
+          const uint32_t ra = (i0 + (lane & 15)) * Cfg::kPK + 32 * kt + 16 * mhi;
+          ldmatrix_x4(qsa + ra, qa);
+          ldmatrix_x4(ksa + ra, ka);
+          ldmatrix_x2(ksa + (8 * kq + mrow) * Cfg::kPK + 32 * kt + 16 * mlo, kb);
+          mma_bf16_16816(qk, qa, kb[0], kb[1]);
+          mma_bf16_16816(kk, ka, kb[0], kb[1]);
+        }
+      }
+    }
+    {      // <S, dS'>
+      const unsigned char *sp = buf + (ssa - at0);
+#pragma unroll
+      for (int x0 = 0; x0 < K * P; x0 += kThreads) {
+        const int x = x0 + tid;
+        if (K * P % kThreads && x >= K * P) break;
+        const uint4 p = *reinterpret_cast<const uint4 *>(sp + 16 * x), d = *reinterpret_cast<const uint4 *>(sp + SB + 16 * x);
         ss = fma_bf16<0, 0>(p.x, d.x, fma_bf16<1, 1>(p.x, d.x, ss));
         ss = fma_bf16<0, 0>(p.y, d.y, fma_bf16<1, 1>(p.y, d.y, ss));
         ss = fma_bf16<0, 0>(p.z, d.z, fma_bf16<1, 1>(p.z, d.z, ss));
         ss = fma_bf16<0, 0>(p.w, d.w, fma_bf16<1, 1>(p.w, d.w, ss));
       }
-      // products over the slab's columns
-      for (int kt = 0; kt < VS / 16; ++kt) {
-        uint32_t ya[4], la[4], ua[4];     // A operands: 16 tokens x 16 columns
-        ldmatrix_x4(ysa + (i0 + mrow + 8 * mlo) * pv + 32 * kt + 16 * mhi, ya);
-        // blocks [column tile][token tile]; transposed: rows are tokens
-        const uint32_t ba = 16 * mrow + 128 * (4 * (2 * kt + mhi) + 2 * mh + mlo);
-        ldmatrix_x4_t(lsa + ba, la);
-        ldmatrix_x4_t(usa + ba, ua);
-        if (kh <= mh) {
-          uint32_t ub[4], wb[4];          // B operands: 16 columns x 16 tokens from 16 kh
-          ldmatrix_x4_t(usa + 16 * mrow + 128 * (4 * (2 * kt + mlo) + 2 * kh + mhi), ub);
-          mma_bf16_16816(yu[0], ya, ub[0], ub[1]);
-          mma_bf16_16816(yu[1], ya, ub[2], ub[3]);
-          mma_bf16_16816(lu[0], la, ub[0], ub[1]);
-          mma_bf16_16816(lu[1], la, ub[2], ub[3]);
-          if (kh == mh) {
-            ldmatrix_x4(vsa + (i0 + mrow + 8 * mhi) * pv + 32 * kt + 16 * mlo, wb);
-            mma_bf16_16816(ld[0], la, wb[0], wb[1]);
-            mma_bf16_16816(ld[1], la, wb[2], wb[3]);
-          }
-        }
-#pragma unroll
-        for (int t = 0; t < NT; t += 2) {
-          // B operands: 16 columns x 16 features (the last pair of an odd number of tiles: the second is not used)
-          const uint32_t fb = f0 / 8 + t + (t + 1 < NT ? mhi : 0);
-          const uint32_t at = 16 * mrow + 128 * ((2 * kt + mlo) * (K / 8) + fb);
-          uint32_t sb[4], db[4];
-          ldmatrix_x4_t(ssa + at, sb);
-          ldmatrix_x4_t(dsa + at, db);
-          mma_bf16_16816(dq[t], ya, sb[0], sb[1]);
-          mma_bf16_16816(dm[t], la, sb[0], sb[1]);
-          mma_bf16_16816(dp[t], ua, db[0], db[1]);
-          if (t + 1 < NT) {
-            mma_bf16_16816(dq[t + 1], ya, sb[2], sb[3]);
-            mma_bf16_16816(dm[t + 1], la, sb[2], sb[3]);
-            mma_bf16_16816(dp[t + 1], ua, db[2], db[3]);
-          }
-        }
-      }
-      if (vb + VS < V) __syncthreads();     // (the slab's place is the next one's)
     }
-    // rows i of this thread: i0 + g, i0 + g + 8
-    const float *vg = vec + 32 * kVecG, *vb_ = vec + 32 * kVecBeta, *vrk = vec + 32 * kVecRk, *vrq = vec + 32 * kVecRq;
-    const float glast = vg[31];
-    float eg[2], ek[2], bt[2], rk[2], rq[2], gi[2];
+    // products over the slab's columns
+    const uint32_t y_at = ysa + (i0 + mrow + 8 * mlo) * pv + 16 * mhi, v_at = vsa + (8 * kq + mrow) * pv + 16 * mlo;
+    const uint32_t b_at = usa + 16 * mrow + 128 * (4 * mhi + 2 * mh + mlo), u_at = usa + 16 * mrow + 128 * (4 * mlo + kq);   // blocks [column tile][token tile]
+    const uint32_t s_at = ssa + 16 * mrow + 128 * (mlo * (K / 8) + f0 / 8 + mhi), s_one = ssa + 16 * mrow + 128 * (mlo * (K / 8) + f0 / 8);
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int i = i0 + g + 8 * x;
-      gi[x] = vg[i]; bt[x] = vb_[i]; rk[x] = vrk[i]; rq[x] = vrq[i];
-      eg[x] = expf(gi[x]);
-      ek[x] = expf(glast - gi[x]);
-    }
-    // q k^T and k k^T, tiles (16 mh, 16 kh)
-    float qk[2][4] = {}, kk[2][4] = {};
-    if (kh <= mh) {
-#pragma unroll
-      for (int kt = 0; kt < K / 16; ++kt) {
-        uint32_t qa[4], ka[4], kb[4];
-        const uint32_t ra = (i0 + (lane & 15)) * Cfg::kPK + 32 * kt + 16 * mhi;
-        ldmatrix_x4(qsa + ra, qa);
-        ldmatrix_x4(ksa + ra, ka);
-        ldmatrix_x4(ksa + (16 * kh + mrow + 8 * mhi) * Cfg::kPK + 32 * kt + 16 * mlo, kb);
-        mma_bf16_16816(qk[0], qa, kb[0], kb[1]);
-        mma_bf16_16816(qk[1], qa, kb[2], kb[3]);
-        mma_bf16_16816(kk[0], ka, kb[0], kb[1]);
-        mma_bf16_16816(kk[1], ka, kb[2], kb[3]);
-      }
-    }
-    float gr[2] = {}, gc[2][2] = {};      // sums of G over this thread's entries of a row, of a column
-    // the four 32 x 32 matrices: 0: s E dP r_k,j   1: s E dP r_q,i   2: E N r_k,j   3: b_i E N r_k,i
-    if (kh <= mh) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int i = i0 + g + 8 * x, j = 16 * kh + 8 * t + 2 * c;
-          const float e0 = i >= j ? __expf(gi[x] - vg[j]) : 0.f, e1 = i >= j + 1 ? __expf(gi[x] - vg[j + 1]) : 0.f;
-          const float p0 = a.scale * e0 * yu[t][2 * x], p1 = a.scale * e1 * yu[t][2 * x + 1];
-          const float m0 = i > j ? -e0 * lu[t][2 * x] : 0.f, m1 = i > j + 1 ? -e1 * lu[t][2 * x + 1] : 0.f;
-          const uint32_t at = mat + 128 * (4 * (2 * mh + x) + 2 * kh + t) + 4 * lane;
-          const float r0 = vrk[j], r1 = vrk[j + 1];
-          const uint32_t w[4] = {pack_bf16(p0 * r0, p1 * r1), pack_bf16(p0 * rq[x], p1 * rq[x]), pack_bf16(m0 * r0, m1 * r1),
-                                 pack_bf16(m0 * bt[x] * rk[x], m1 * bt[x] * rk[x])};
-#pragma unroll
-          for (int m = 0; m < 4; ++m) sts32(at + 2048 * m, __uint_as_float(w[m]));
-          const float b = bt[x] * rk[x];
-          const float t0 = i > j ? r0 * fmaf(p0 * rq[x], qk[t][2 * x], m0 * b * kk[t][2 * x]) : 0.f;
-          const float t1 = i > j + 1 ? r1 * fmaf(p1 * rq[x], qk[t][2 * x + 1], m1 * b * kk[t][2 * x + 1]) : 0.f;
-          gr[x] += t0 + t1;
-          gc[t][0] += t0;
-          gc[t][1] += t1;
-        }
-      if (kh == mh)      // L_i . v_i: the diagonal
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (g + 8 * (r >> 1) == 8 * t + 2 * c + (r & 1)) lv[i0 + g + 8 * (r >> 1)] = ld[t][r];
-    }
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      gr[x] += __shfl_xor_sync(0xffffffffu, gr[x], 1);
-      gr[x] += __shfl_xor_sync(0xffffffffu, gr[x], 2);
-      if (c == 0) grow[32 * kh + i0 + g + 8 * x] = gr[x];
-    }
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-#pragma unroll
-        for (int d = 4; d < 32; d *= 2) gc[t][e] += __shfl_xor_sync(0xffffffffu, gc[t][e], d);
-        if (g == 0) gcol[32 * mh + 16 * kh + 8 * t + 2 * c + e] = gc[t][e];
-      }
-    // the parts from S and dS' scaled; W and R
-    float d0[2] = {}, dr[2] = {};
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const float sq = a.scale * eg[x];
-        dq[t][2 * x] *= sq; dq[t][2 * x + 1] *= sq;
-        dm[t][2 * x] *= -eg[x]; dm[t][2 * x + 1] *= -eg[x];
-        dp[t][2 * x] *= ek[x]; dp[t][2 * x + 1] *= ek[x];
-        const float2 kv = unpack_bf16(__float_as_uint(lds32(kat + 8 * x * Cfg::kPK + 16 * t))), qv = unpack_bf16(__float_as_uint(lds32(qat + 8 * x * Cfg::kPK + 16 * t)));
-        const float b = bt[x] * rk[x];
-        d0[x] = fmaf(kv.x, dp[t][2 * x], fmaf(kv.y, dp[t][2 * x + 1], d0[x]));
-        dr[x] = fmaf(rq[x], fmaf(qv.x, dq[t][2 * x], qv.y * dq[t][2 * x + 1]), fmaf(b, fmaf(kv.x, dm[t][2 * x], kv.y * dm[t][2 * x + 1]), dr[x]));
-      }
-    __syncthreads();
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      // rows of this warp's tokens against tokens 16 kt (k-tile): lower for dQ^, dK-, its transpose for dK+
-      const bool lo = kt <= mh, up = kt >= mh;
-      uint32_t m0[4], m1[4], m2[4], m3[4];
-      if (lo) {
-        const uint32_t at = mat + 16 * mrow + 128 * (4 * (2 * mh + mlo) + 2 * kt + mhi);
-        ldmatrix_x4(at, m0);
-        ldmatrix_x4(at + 2 * 2048, m2);
-      }
-      if (up) {
-        const uint32_t at = mat + 16 * mrow + 128 * (4 * (2 * kt + mhi) + 2 * mh + mlo);
-        ldmatrix_x4_t(at + 2048, m1);
-        ldmatrix_x4_t(at + 3 * 2048, m3);
+    for (int kt = 0; kt < VS / 16; ++kt) {
+      uint32_t ya[4], la[4], ua[4];     // A operands: 16 tokens x 16 columns
+      ldmatrix_x4(y_at + 32 * kt, ya);
+      ldmatrix_x4_t(b_at + 1024 * kt, ua);
+      ldmatrix_x4_t(b_at + UB + 1024 * kt, la);
+      if (low) {
+        uint32_t ub[2], wb[2];          // B operands: 16 columns x 8 tokens from 8 kq
+        ldmatrix_x2_t(u_at + 1024 * kt, ub);
+        mma_bf16_16816(yu, ya, ub[0], ub[1]);
+        mma_bf16_16816(lu, la, ub[0], ub[1]);
+        ldmatrix_x2(v_at + 32 * kt, wb);      // (needed on the diagonal alone)
+        mma_bf16_16816(ld, la, wb[0], wb[1]);
       }
 #pragma unroll
       for (int t = 0; t < NT; t += 2) {
-        const uint32_t at = (16 * kt + mrow + 8 * mlo) * Cfg::kPK + 2 * f0 + 16 * (t + (t + 1 < NT ? mhi : 0));
-        uint32_t kb[4], qb[4];
-        ldmatrix_x4_t(ksa + at, kb);
-        if (up) ldmatrix_x4_t(qsa + at, qb);
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          if (t + e < NT) {
-            if (lo) {
-              mma_bf16_16816(dq[t + e], m0, kb[2 * e], kb[2 * e + 1]);
-              mma_bf16_16816(dm[t + e], m2, kb[2 * e], kb[2 * e + 1]);
-            }
-            if (up) {
-              mma_bf16_16816(dp[t + e], m1, qb[2 * e], qb[2 * e + 1]);
-              mma_bf16_16816(dp[t + e], m3, kb[2 * e], kb[2 * e + 1]);
-            }
-          }
+        // B operands: 16 columns x 16 features (of a last tile alone the second is not used)
+        if (t >= tiles) continue;
+        const uint32_t at = (t + 1 < tiles ? s_at : s_one) + 32 * K * kt + 128 * t;
+        uint32_t sb[4], db[4];
+        ldmatrix_x4_t(at, sb);
+        ldmatrix_x4_t(at + SB, db);
+        mma_bf16_16816(dq[t], ya, sb[0], sb[1]);
+        mma_bf16_16816(dm[t], la, sb[0], sb[1]);
+        mma_bf16_16816(dp[t], ua, db[0], db[1]);
+        if (t + 1 < NT && t + 1 < tiles) {
+          mma_bf16_16816(dq[t + 1], ya, sb[2], sb[3]);
+          mma_bf16_16816(dm[t + 1], la, sb[2], sb[3]);
+          mma_bf16_16816(dp[t + 1], ua, db[2], db[3]);
+        }
       }
     }
-    // sums over the features: q . dQ^, k . dK-, k . dK+ and the two above, then over the two halves of the features
-    float d1[2] = {}, d2[2] = {}, d3[2] = {};
+    }
+    // rows i of this thread: i0 + g, i0 + g + 8
+    float bt[2], eq[2], egk[2], ek[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int i = i0 + g + 8 * x;
+      bt[x] = vec[32 * kVecBeta + i]; eq[x] = vec[32 * kVecEq + i]; egk[x] = vec[32 * kVecEgk + i]; ek[x] = vec[32 * kVecEk + i];
+    }
+    if (low) {
+      const int j = 8 * kq + 2 * c;
+      const float2 gj = *reinterpret_cast<const float2 *>(vec + 32 * kVecG + j), rj = *reinterpret_cast<const float2 *>(vec + 32 * kVecRk + j);
+      float c0 = 0.f, c1 = 0.f;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int i = i0 + g + 8 * x;
+        const float gi = vec[32 * kVecG + i], rk = vec[32 * kVecRk + i], rq = a.scale * vec[32 * kVecRq + i];
+        const float e0 = i >= j ? __expf(gi - gj.x) * rj.x : 0.f, e1 = i > j ? __expf(gi - gj.y) * rj.y : 0.f;
+        const float x10 = rq * e0 * yu[2 * x], x11 = rq * e1 * yu[2 * x + 1];
+        const float n0_ = i > j ? -rk * e0 * lu[2 * x] : 0.f, n1_ = i > j + 1 ? -rk * e1 * lu[2 * x + 1] : 0.f;
+        const uint32_t at = mat + 128 * (4 * (2 * mh + x) + kq) + 4 * lane;
+        sts32(at, __uint_as_float(pack_bf16(x10, x11)));
+        sts32(at + 2048, __uint_as_float(pack_bf16(bt[x] * n0_, bt[x] * n1_)));
+        const float t0 = x10 * qk[2 * x], t1 = x11 * qk[2 * x + 1], u0 = n0_ * kk[2 * x], u1 = n1_ * kk[2 * x + 1];
+        c0 += fmaf(bt[x], u0, i > j ? t0 : 0.f);
+        c1 += fmaf(bt[x], u1, i > j + 1 ? t1 : 0.f);
+        if (i == j) { red[32 * kDiag + i] = t0; red[32 * kLv + i] = ld[2 * x]; }
+        if (i == j + 1) { red[32 * kDiag + i] = t1; red[32 * kLv + i] = ld[2 * x + 1]; }
+        float r1 = t0 + t1, r2 = u0 + u1;
+        r1 += __shfl_xor_sync(0xffffffffu, r1, 1);
+        r2 += __shfl_xor_sync(0xffffffffu, r2, 1);
+        r1 += __shfl_xor_sync(0xffffffffu, r1, 2);
+        r2 += __shfl_xor_sync(0xffffffffu, r2, 2);
+        if (c == 0) { red[32 * (kRow1 + kq) + i] = r1; red[32 * (kRow2 + kq) + i] = r2; }
+      }
+#pragma unroll
+      for (int d = 4; d < 32; d *= 2) {
+        c0 += __shfl_xor_sync(0xffffffffu, c0, d);
+        c1 += __shfl_xor_sync(0xffffffffu, c1, d);
+      }
+      if (g == 0) *reinterpret_cast<float2 *>(red + 32 * (kCol + mh) + j) = make_float2(c0, c1);
+    } else {      // (16 mh, 8 kq) above the diagonal: nothing to add
+      if (c == 0) red[32 * (kRow1 + kq) + i0 + g] = red[32 * (kRow1 + kq) + i0 + g + 8] = red[32 * (kRow2 + kq) + i0 + g] = red[32 * (kRow2 + kq) + i0 + g + 8] = 0.f;
+      if (g == 0) *reinterpret_cast<float2 *>(red + 32 * (kCol + mh) + 8 * kq + 2 * c) = make_float2(0.f, 0.f);
+    }
+    // a1, a2, a3; the products with the states scaled and put together
+    uint32_t qw[NT][2], kw[NT][2];
+    float a1[2] = {}, a2[2] = {}, a3[2] = {};
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const float2 qv = unpack_bf16(__float_as_uint(lds32(qat + 8 * x * Cfg::kPK + 16 * t))), kv = unpack_bf16(__float_as_uint(lds32(kat + 8 * x * Cfg::kPK + 16 * t)));
-        d1[x] = fmaf(qv.x, dq[t][2 * x], fmaf(qv.y, dq[t][2 * x + 1], d1[x]));
-        d2[x] = fmaf(kv.x, dm[t][2 * x], fmaf(kv.y, dm[t][2 * x + 1], d2[x]));
-        d3[x] = fmaf(kv.x, dp[t][2 * x], fmaf(kv.y, dp[t][2 * x + 1], d3[x]));
+        if (t >= tiles) continue;
+        qw[t][x] = __float_as_uint(lds32(qat + 8 * x * Cfg::kPK + 16 * t));
+        kw[t][x] = __float_as_uint(lds32(kat + 8 * x * Cfg::kPK + 16 * t));
+        const float2 qv = unpack_bf16(qw[t][x]), kv = unpack_bf16(kw[t][x]);
+        a1[x] = fmaf(qv.x, dq[t][2 * x], fmaf(qv.y, dq[t][2 * x + 1], a1[x]));
+        a2[x] = fmaf(kv.x, dm[t][2 * x], fmaf(kv.y, dm[t][2 * x + 1], a2[x]));
+        a3[x] = fmaf(kv.x, dp[t][2 * x], fmaf(kv.y, dp[t][2 * x + 1], a3[x]));
+        const float be = -bt[x] * egk[x];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          dq[t][2 * x + e] *= eq[x];
+          dm[t][2 * x + e] = fmaf(be, dm[t][2 * x + e], ek[x] * dp[t][2 * x + e]);
+        }
       }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      float *v5[5] = {&d0[x], &d1[x], &d2[x], &d3[x], &dr[x]};
-#pragma unroll
-      for (int y = 0; y < 5; ++y) {
-        float &v = *v5[y];
-        v += __shfl_xor_sync(0xffffffffu, v, 1);
-        v += __shfl_xor_sync(0xffffffffu, v, 2);
-        v *= y == 4 ? 1.f : y == 1 ? rq[x] : rk[x];
-        if (c == 0) red[(2 * y + kh) * 32 + i0 + g + 8 * x] = v;
-      }
+      a1[x] += __shfl_xor_sync(0xffffffffu, a1[x], 1);
+      a2[x] += __shfl_xor_sync(0xffffffffu, a2[x], 1);
+      a3[x] += __shfl_xor_sync(0xffffffffu, a3[x], 1);
+      a1[x] += __shfl_xor_sync(0xffffffffu, a1[x], 2);
+      a2[x] += __shfl_xor_sync(0xffffffffu, a2[x], 2);
+      a3[x] += __shfl_xor_sync(0xffffffffu, a3[x], 2);
+      if (c < 3) red[32 * (kA + 4 * c + kq) + i0 + g + 8 * x] = c == 0 ? a1[x] : c == 1 ? a2[x] : a3[x];
     }
 #pragma unroll
     for (int d = 16; d; d /= 2) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-    if (lane == 0) sds[warp] = ss;
+    if (lane == 0) red[32 * kSds + warp] = ss;
     __syncthreads();
-    if (warp == 0) {
-      const float w = red[lane] + red[32 + lane], e2 = red[128 + lane] + red[160 + lane], r = red[256 + lane] + red[288 + lane];
-      float all = w, part = r + grow[lane] + grow[32 + lane] - w - gcol[lane] - gcol[32 + lane];
+    if (warp == 0) {      // a token a lane
+      auto sum4 = [&](int r) { const float *p = red + 32 * r + lane; return (p[0] + p[32]) + (p[64] + p[96]); };
+      const float b = vec[32 * kVecBeta + lane], rk = vec[32 * kVecRk + lane], rq = vec[32 * kVecRq + lane];
+      const float s1 = vec[32 * kVecEq + lane] * sum4(kA), s2 = vec[32 * kVecEgk + lane] * sum4(kA + 4), W = vec[32 * kVecEk + lane] * sum4(kA + 8);
+      const float r1 = sum4(kRow1), r2 = sum4(kRow2), col = red[32 * kCol + lane] + red[32 * kCol + 32 + lane], diag = red[32 * kDiag + lane];
+      const float pq = s1 + r1, pk = fmaf(b, r2 - s2, W + col + diag);      // q . dq', k . dk'
+      red[32 * kUq + lane] = a.qk_norm ? -rq * rq * pq : 0.f;
+      red[32 * kUk + lane] = a.qk_norm ? -rk * rk * pk : 0.f;
+      float all = W, part = s1 + (r1 - diag) + b * (r2 - s2) - W - col;
 #pragma unroll
       for (int d = 16; d; d /= 2) all += __shfl_xor_sync(0xffffffffu, all, d);
 #pragma unroll
@@ -333,56 +350,97 @@ __global__ void __launch_bounds__(128, 2) delta_grad_kernel(DeltaArgs a) {
         const float o = __shfl_down_sync(0xffffffffu, part, d);
         if (lane + d < 32) part += o;
       }
-      if (lane < have) {
-        const size_t at = (size_t)(tok + lane) * a.N + n;
-        const float dlog = part + all + expf(glast) * (sds[0] + sds[1] + sds[2] + sds[3]);
-        float ds;
-        (void)delta_step_of(a.step_kind, __bfloat162float(static_cast<const __nv_bfloat16 *>(a.step)[at]), ds);
+      if (lane < o.have) {
+        const size_t at = (size_t)(o.tok + lane) * a.N + n;
+        const float4 p = *reinterpret_cast<const float4 *>(red + 32 * kSds), q = *reinterpret_cast<const float4 *>(red + 32 * kSds + 4);
+        const float dlog = part + all + expf(vec[32 * kVecG + 31]) * (((p.x + p.y) + (p.z + p.w)) + ((q.x + q.y) + (q.z + q.w)));
         static_cast<__nv_bfloat16 *>(a.dgate)[at] = __float2bfloat16_rn(dlog * vec[32 * kVecDlog + lane]);
-        static_cast<__nv_bfloat16 *>(a.dstep)[at] = __float2bfloat16_rn((lv[lane] + e2) * ds);
+        static_cast<__nv_bfloat16 *>(a.dstep)[at] = __float2bfloat16_rn((red[32 * kLv + lane] - s2 + r2) * (a.step_kind == M2RNN_STEP_LOGIT ? b * (1.f - b) : 1.f));
       }
     }
-    // through the division by the lengths: dx = r (dx^ - x^ (x^ . dx^))
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      // rows of this warp's tokens against tokens 16 kt (k-tile): lower parts, and transposed ones
+      const bool lo = kt <= mh, up = kt >= mh;
+      uint32_t x1[4], x2[4], t1[4], t2[4];
+      if (lo) {
+        const uint32_t at = mat + 16 * mrow + 128 * (4 * (2 * mh + mlo) + 2 * kt + mhi);
+        ldmatrix_x4(at, x1);
+        ldmatrix_x4(at + 2048, x2);
+      }
+      if (up) {
+        const uint32_t at = mat + 16 * mrow + 128 * (4 * (2 * kt + mhi) + 2 * mh + mlo);
+        ldmatrix_x4_t(at, t1);
+        ldmatrix_x4_t(at + 2048, t2);
+      }
+#pragma unroll
+      for (int t = 0; t < NT; t += 2) {
+        if (t >= tiles) continue;
+        const uint32_t at = (16 * kt + mrow + 8 * mlo) * Cfg::kPK + 2 * f0 + 16 * (t + (t + 1 < tiles ? mhi : 0));
+        uint32_t kb[4], qb[4];
+        ldmatrix_x4_t(ksa + at, kb);
+        if (up) ldmatrix_x4_t(qsa + at, qb);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (t + e < NT) {
+            if (t + e >= tiles) continue;
+            if (lo) {
+              mma_bf16_16816(dq[t + e], x1, kb[2 * e], kb[2 * e + 1]);
+              mma_bf16_16816(dm[t + e], x2, kb[2 * e], kb[2 * e + 1]);
+            }
+            if (up) {
+              mma_bf16_16816(dm[t + e], t1, qb[2 * e], qb[2 * e + 1]);
+              mma_bf16_16816(dm[t + e], t2, kb[2 * e], kb[2 * e + 1]);
+            }
+          }
+      }
+    }
+    __syncthreads();      // the factors are there; X1, X2 and (at the last head) q and k are read
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const int i = i0 + g + 8 * x;
-      float pq = 0.f, pk = 0.f;
-      if (a.qk_norm) {
-        pq = red[64 + i] + red[96 + i];
-        pk = bt[x] * (red[128 + i] + red[160 + i]) + red[192 + i] + red[224 + i];
-      }
-      const float uq = -pq * rq[x] * rq[x], uk = -pk * rk[x] * rk[x];
+      const float uq = red[32 * kUq + i0 + g + 8 * x], uk = red[32 * kUk + i0 + g + 8 * x];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const float2 qv = unpack_bf16(__float_as_uint(lds32(qat + 8 * x * Cfg::kPK + 16 * t))), kv = unpack_bf16(__float_as_uint(lds32(kat + 8 * x * Cfg::kPK + 16 * t)));
-        const float q0 = fmaf(uq, qv.x, rq[x] * dq[t][2 * x]), q1 = fmaf(uq, qv.y, rq[x] * dq[t][2 * x + 1]);
-        const float k0 = fmaf(uk, kv.x, rk[x] * fmaf(bt[x], dm[t][2 * x], dp[t][2 * x])), k1 = fmaf(uk, kv.y, rk[x] * fmaf(bt[x], dm[t][2 * x + 1], dp[t][2 * x + 1]));
-        if constexpr (MULTI) {
-          dqs[t][2 * x] += q0; dqs[t][2 * x + 1] += q1;
-          dks[t][2 * x] += k0; dks[t][2 * x + 1] += k1;
-        } else {
-          dq[t][2 * x] = q0; dq[t][2 * x + 1] = q1;
-          dm[t][2 * x] = k0; dm[t][2 * x + 1] = k1;
-        }
+        if (t >= tiles) continue;
+        const float2 qv = unpack_bf16(qw[t][x]), kv = unpack_bf16(kw[t][x]);
+        dq[t][2 * x] = fmaf(uq, qv.x, dq[t][2 * x]);
+        dq[t][2 * x + 1] = fmaf(uq, qv.y, dq[t][2 * x + 1]);
+        dm[t][2 * x] = fmaf(uk, kv.x, dm[t][2 * x]);
+        dm[t][2 * x + 1] = fmaf(uk, kv.y, dm[t][2 * x + 1]);
+        if constexpr (MULTI)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            dqs[t][2 * x + e] += dq[t][2 * x + e];
+            dks[t][2 * x + e] += dm[t][2 * x + e];
+          }
       }
     }
-    __syncthreads();      // the vectors, matrices and sums are read, and (at the last head) q and k
     if constexpr (!MULTI) emit(dq, dm);
   }
   if constexpr (MULTI) emit(dqs, dks);
   __syncthreads();
-  for (int x = tid; x < have * (K / 8); x += 128) {
-    const int r = x / (K / 8), o = x % (K / 8);
-    if (!a.dq_part) *reinterpret_cast<float4 *>(static_cast<__nv_bfloat16 *>(a.dq) + ((size_t)(tok + r) * a.Nq + hq) * K + 8 * o) = lds128(qsa + r * Cfg::kPK + 16 * o);
-    if (!a.dk_part) *reinterpret_cast<float4 *>(static_cast<__nv_bfloat16 *>(a.dk) + ((size_t)(tok + r) * a.Nk + hk) * K + 8 * o) = lds128(ksa + r * Cfg::kPK + 16 * o);
+  for (int x = tid; x < o.have * (K / 8); x += kThreads) {
+    const int r = x / (K / 8), p = x % (K / 8);
+    if (!a.dq_part) *reinterpret_cast<float4 *>(static_cast<__nv_bfloat16 *>(a.dq) + ((size_t)(o.tok + r) * a.Nq + o.hq) * K + 8 * p) = lds128(qsa + r * Cfg::kPK + 16 * p);
+    if (!a.dk_part) *reinterpret_cast<float4 *>(static_cast<__nv_bfloat16 *>(a.dk) + ((size_t)(o.tok + r) * a.Nk + o.hk) * K + 8 * p) = lds128(ksa + r * Cfg::kPK + 16 * p);
+  }
+  if (!next.have) break;
+  o = next;
   }
 }
 
-template <int K, bool MULTI> cudaError_t launch_km(const DeltaArgs &a, cudaStream_t s) {
-  const size_t smem = GradCfg<K>::kSlab + slab_bytes(K, a.V < 64 ? a.V : 64);
-  const cudaError_t e = allow_smem(delta_grad_kernel<K, MULTI>, smem);
+template <int K, bool MULTI, int VS> cudaError_t launch_kmv(const DeltaArgs &a, cudaStream_t s) {
+  constexpr size_t smem = GradCfg<K>::kSlab + 2 * (size_t)slab_bytes(K, VS);
+  static_assert(smem <= 113 * 1024, "two CTAs to an SM");
+  const cudaError_t e = allow_smem(delta_grad_kernel<K, MULTI, VS>, smem);
   if (e != cudaSuccess) return e;
-  return launch_early(delta_grad_kernel<K, MULTI>, dim3((unsigned)((long long)a.B * a.nch * (a.N / a.hpc))), dim3(128), smem, s, a);
+  const unsigned jobs = (unsigned)((long long)a.B * a.nch * (a.N / a.hpc)), most = 2 * (unsigned)sm_count();
+  return launch_early(delta_grad_kernel<K, MULTI, VS>, dim3(jobs < most ? jobs : most), dim3(kThreads), smem, s, a, jobs);
+}
+template <int K, bool MULTI> cudaError_t launch_km(const DeltaArgs &a, cudaStream_t s) {
+  if (a.V == 16) return launch_kmv<K, MULTI, 16>(a, s);
+  if (a.V == 32 || GradCfg<K>::VS == 32) return launch_kmv<K, MULTI, 32>(a, s);
+  return launch_kmv<K, MULTI, GradCfg<K>::VS>(a, s);
 }
 template <int K> cudaError_t launch_k(const DeltaArgs &a, cudaStream_t s) { return a.hpc > 1 ? launch_km<K, true>(a, s) : launch_km<K, false>(a, s); }
 
