@@ -15,8 +15,9 @@
 // (With q . dq - k . dk in place of R, W and G the pairs on one side of t would cancel only up to the roundings of
 // the matrices to bf16: 2.5e-2 off where states decay within a few tokens.  Here the same fp32 value is added and taken away.)
 //
-// Eight warps: 16 tokens x a quarter of the K features each; the products over V in slabs of 64 columns (32 where K > 64).
-// A job is a chunk of `hpc` heads that share q and k, one after the other, their dq and dk added up in registers.  Two CTAs
+// 2 KG warps: 16 tokens x one of KG parts of the K features each; the products over V in slabs of 64 columns (32 where K > 64).
+// A job is a chunk of `hpc` heads that share q and k, one after the other: their X1, X2, dq', dk' are added up in registers, and the products
+// with Q and K, which are the same for all of them, taken once.  Two CTAs
 // to an SM walk over the jobs, the next slab (and the next job's rows) on its way while one is worked on: with a CTA a job the
 // loads' latency stood between a third of the cycles.  What the chains wrote is contiguous and comes by untiled bulk
 // copies; rows of q, k, v and dY by cp.async.
@@ -25,29 +26,31 @@
 namespace m2rnn {
 namespace {
 
-constexpr int C = kDeltaChunk, kThreads = 256;
+constexpr int C = kDeltaChunk;
 
-template <int K> struct GradCfg {
+template <int K, int KG> struct GradCfg {
+  static constexpr int kThreads = 64 * KG;
   static constexpr int kPK = 2 * K + 16;
   static constexpr int kRows = 2 * C * kPK, kMat = 2 * kRows;            // q, k rows, twice; X1, X2 as blocks
   static constexpr int kRed = kMat + 2 * 2048;                           // sums, see Red
-  static constexpr int kSlab = kRed + 27 * 128 + 128;                    // slabs: the vectors, dY, V rows, then U, L, S, dS' blocks
-  static constexpr int NT = (K + 31) / 32;                               // 8-feature tiles of a warp, most
-  static constexpr int VS = K > 64 ? 32 : 64;                            // columns of a slab, most
+  static constexpr int kSlab = kRed + (5 * KG + 7) * 128;                // slabs: the vectors, dY, V rows, then U, L, S, dS' blocks
+  static constexpr int NT = (K / 8 + KG - 1) / KG;                       // 8-feature tiles of a warp, most
+  static constexpr int JT = 4 / KG;                                      // 8-token tiles of a warp's part of a 16 x 32 product
+  // rows of 32 floats: a1, a2, a3 by part of the features; sums of X1 (.) QK^T and X2 (.) KK^T / b over a row's entries by part of
+  // the tokens; over a column's by half; X1 (.) QK^T's diagonal; L . v; the factors of the division by the lengths; <S, dS'> by warp
+  static constexpr int kA = 0, kRow1 = 3 * KG, kRow2 = 4 * KG, kCol = 5 * KG, kDiag = kCol + 2, kLv = kCol + 3, kUq = kCol + 4, kUk = kCol + 5, kSds = kCol + 6;
   static_assert(kSlab % 16 == 0, "");
 };
-// rows of 32 floats: a1, a2, a3 by quarter; sums of X1 (.) QK^T and X2 (.) KK^T / b over a row's entries by quarter; over a
-// column's by half; X1 (.) QK^T's diagonal; L . v; the factors of the division by the lengths; <S, dS'> by warp
-enum Red { kA = 0, kRow1 = 12, kRow2 = 16, kCol = 20, kDiag = 22, kLv = 23, kUq = 24, kUk = 25, kSds = 26 };
 __host__ __device__ constexpr int slab_bytes(int K, int VS) { return 1024 + 2 * C * (2 * VS + 16) + 2 * 2 * C * VS + 2 * 2 * K * VS; }
 
 struct GradJob { long long tok; size_t slot; int have, n0, run, hq, hk; };      // have = 0: no more
 
 // MULTI: several heads to a job; VS: columns of a slab
-template <int K, bool MULTI, int VS>
-__global__ void __launch_bounds__(kThreads, 2) delta_grad_kernel(DeltaArgs a, unsigned jobs) {
-  using Cfg = GradCfg<K>;
-  constexpr int NT = Cfg::NT;
+template <int K, int KG, bool MULTI, int VS, int BUFS, int CTAS>
+__global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, unsigned jobs) {
+  using Cfg = GradCfg<K, KG>;
+  constexpr int NT = Cfg::NT, JT = Cfg::JT, kThreads = Cfg::kThreads;
+  constexpr int pv = 2 * VS + 16, P = VS / 8, slab = slab_bytes(K, VS), UB = 2 * C * VS, SB = 2 * K * VS;      // P: pieces of a row; bytes of U, of S
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ uint64_t full[2];
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = tid & 31, g = lane >> 2, c = lane & 3;
@@ -57,9 +60,7 @@ __global__ void __launch_bounds__(kThreads, 2) delta_grad_kernel(DeltaArgs a, un
     fence_mbar_init();
   }
   const int mh = warp & 1, kq = warp >> 1, i0 = 16 * mh, f0 = 8 * NT * kq;      // tokens i0 .., features f0 ..
-  const int tiles = K % 32 == 0 ? NT : min(NT, max(0, K / 8 - NT * kq));        // 8-feature tiles that this warp has
-  const bool low = kq <= 2 * mh + 1;                                            // tile (16 mh, 8 kq) of 32 x 32: not above the diagonal's blocks
-  constexpr int pv = 2 * VS + 16, P = VS / 8, slab = slab_bytes(K, VS), UB = 2 * C * VS, SB = 2 * K * VS;      // P: pieces of a row; bytes of U, of S
+  const int tiles = K % (8 * KG) == 0 ? NT : min(NT, max(0, K / 8 - NT * kq));  // 8-feature tiles that this warp has
   const int V = a.V, parts = (unsigned)V / VS;
   const uint32_t base = smem_u32(smem), mat = base + Cfg::kMat;
   float *red = reinterpret_cast<float *>(smem + Cfg::kRed);
@@ -111,12 +112,15 @@ __global__ void __launch_bounds__(kThreads, 2) delta_grad_kernel(DeltaArgs a, un
       bulk_load(usa + 2 * UB, a.states + x, SB, full + buf);
       bulk_load(usa + 2 * UB + SB, a.dstates + x, SB, full + buf);
     }
-    if (tid < C * P) {      // (one piece a thread: P <= 8)
-      const int r = tid / P, p = tid % P;
+    const __nv_bfloat16 *yg = static_cast<const __nv_bfloat16 *>(a.dy) + (o.tok * a.N + n) * V + vb, *vg = static_cast<const __nv_bfloat16 *>(a.v) + o.tok * a.vs + (long long)n * V + vb;
+    const long long ys = (long long)a.N * V;
+#pragma unroll
+    for (int x0 = 0; x0 < C * P; x0 += kThreads) {
+      const int x = x0 + tid, r = x / P, p = x % P;
+      if (C * P % kThreads && x >= C * P) break;
       const bool ok = r < o.have;
-      const long long t = o.tok + (ok ? r : 0), col = (long long)n * V + vb + 8 * p;
-      cp16_or_zero(ysa + r * pv + 16 * p, static_cast<const __nv_bfloat16 *>(a.dy) + t * a.N * V + col, ok);
-      cp16_or_zero(vsa + r * pv + 16 * p, static_cast<const __nv_bfloat16 *>(a.v) + t * a.vs + col, ok);
+      cp16_or_zero(ysa + r * pv + 16 * p, yg + (ok ? r * ys : 0) + 8 * p, ok);
+      cp16_or_zero(vsa + r * pv + 16 * p, vg + (ok ? r * a.vs : 0) + 8 * p, ok);
     }
   };
   unsigned j = blockIdx.x;
@@ -126,236 +130,246 @@ __global__ void __launch_bounds__(kThreads, 2) delta_grad_kernel(DeltaArgs a, un
   fetch(o, o.n0, 0, 0);
   bool fine = true;
   unsigned cnt = 0;      // slabs so far: the buffer's parity and its barrier's phase
+  float qk[JT][4], kk[JT][4];                 // q k^T and k k^T, tiles (16 mh, 8 (JT kq + u))
+  float dq[NT][4], dm[NT][4], dp[NT][4];      // dY S^T, L S^T, U dS'^T
+  float yu[JT][4], lu[JT][4], ld[JT][4];      // dY U^T, L U^T, L V^T, tiles as of qk
+  float dqs[NT][4], dks[NT][4], x1s[JT][4], x2s[JT][4];      // dq', dk', X1, X2, summed over a job's heads
+  float pqs = 0.f, pks = 0.f;                 // (warp 0) of q . dq', k . dk'
   for (int qb = 0;; qb ^= 1) {
-  const uint32_t qsa = base + qb * Cfg::kRows, ksa = qsa + C * Cfg::kPK, qat = qsa + (i0 + g) * Cfg::kPK + 2 * (f0 + 2 * c), kat = qat + C * Cfg::kPK;   // (at: this thread's entries)
-  GradJob next{};
-
-  // results: to their shares, or to the places of q and k
-  auto emit_to = [&](const float (&x)[NT][4], float *part, uint32_t at) {
-    if (part) {
-      part += ((size_t)(o.tok + i0 + g) * a.shares + o.run) * K + f0 + 2 * c;
+    const uint32_t qsa = base + qb * Cfg::kRows, ksa = qsa + C * Cfg::kPK, qat = qsa + (i0 + g) * Cfg::kPK + 2 * (f0 + 2 * c), kat = qat + C * Cfg::kPK;   // (at: this thread's entries)
+    GradJob next{};
+    for (int h = 0; h < a.hpc; ++h) {
+      const int n = o.n0 + h;
 #pragma unroll
-      for (int h = 0; h < 2; ++h, part += (size_t)8 * a.shares * K)
-        if (i0 + g + 8 * h < o.have)
+      for (int r = 0; r < 4; ++r) {
 #pragma unroll
-          for (int t = 0; t < NT; ++t)
-            if (t < tiles) *reinterpret_cast<float2 *>(part + 8 * t) = make_float2(x[t][2 * h], x[t][2 * h + 1]);
-    } else {
+        for (int u = 0; u < JT; ++u) yu[u][r] = lu[u][r] = ld[u][r] = 0.f;
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          if (t < tiles) sts32(at + 8 * h * Cfg::kPK + 16 * t, __uint_as_float(pack_bf16(x[t][2 * h], x[t][2 * h + 1])));
-    }
-  };
-  auto emit = [&](const float (&oq)[NT][4], const float (&ok)[NT][4]) { emit_to(oq, a.dq_part, qat); emit_to(ok, a.dk_part, kat); };
-  float dqs[MULTI ? NT : 1][4], dks[MULTI ? NT : 1][4];
-  if constexpr (MULTI)
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) dqs[t][r] = dks[t][r] = 0.f;
-  float qk[4], kk[4];                         // q k^T and k k^T, tile (16 mh, 8 kq)
-  float dq[NT][4], dm[NT][4], dp[NT][4];      // dY S^T, L S^T, U dS'^T; then dq', dk'
-  float yu[4], lu[4], ld[4];                  // tiles (16 mh, 8 kq): dY U^T, L U^T, L V^T
-  float ss;                                   // this thread's part of <S, dS'>
-  for (int h = 0; h < a.hpc; ++h) {
-    const int n = o.n0 + h;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      yu[r] = lu[r] = ld[r] = 0.f;
-#pragma unroll
-      for (int t = 0; t < NT; ++t) dq[t][r] = dm[t][r] = dp[t][r] = 0.f;
-    }
-    ss = 0.f;
-    const float *vec = nullptr;
-    for (int part = 0; part < parts; ++part, ++cnt) {
-    const int bi = cnt & 1;
-    cp_wait_all();
-    if (fine) {      // (after a wait that ran out the rest is worked through with whatever there is: every access is in bounds)
-      fine = mbar_wait(full + bi, (cnt >> 1) & 1);
-      if (!fine && lane == 0) report_timeout(a.dev_status);
-    }
-    __syncthreads();
-    if (part + 1 < parts) fetch(o, n, part + 1, bi ^ 1);
-    else if (h + 1 < a.hpc) fetch(o, n + 1, 0, bi ^ 1);
-    else {
-      j += gridDim.x;
-      next = find(j);
-      if (next.have) {
-        fetch_rows(next, qb ^ 1);
-        fetch(next, next.n0, 0, bi ^ 1);
+        for (int t = 0; t < NT; ++t) dq[t][r] = dm[t][r] = dp[t][r] = 0.f;
       }
-    }
-    unsigned char *buf = smem + Cfg::kSlab + bi * slab;
-    const uint32_t at0 = base + Cfg::kSlab + bi * slab, ysa = at0 + 1024, vsa = ysa + C * pv, usa = vsa + C * pv, ssa = usa + 2 * UB;
-    vec = reinterpret_cast<const float *>(buf);
-    if (h == 0 && part == 0) {
+      float ss = 0.f;      // this thread's part of <S, dS'>
+      const float *vec = nullptr;
+      for (int part = 0; part < parts; ++part, ++cnt) {
+        const int bi = BUFS > 1 ? cnt & 1 : 0;
+        cp_wait_all();
+        if (fine) {      // (after a wait that ran out the rest is worked through with whatever there is: every access is in bounds)
+          fine = mbar_wait(full + bi, (BUFS > 1 ? cnt >> 1 : cnt) & 1);
+          if (!fine && lane == 0) report_timeout(a.dev_status);
+        }
+        __syncthreads();
+        if (BUFS > 1 && part + 1 < parts) fetch(o, n, part + 1, bi ^ 1);
+        else if (BUFS > 1 && h + 1 < a.hpc) fetch(o, n + 1, 0, bi ^ 1);
+        else if (part + 1 == parts && h + 1 == a.hpc) {
+          j += gridDim.x;
+          next = find(j);
+          if (next.have) {
+            fetch_rows(next, qb ^ 1);
+            if (BUFS > 1) fetch(next, next.n0, 0, bi ^ 1);
+          }
+        }
+        unsigned char *buf = smem + Cfg::kSlab + bi * slab;
+        const uint32_t at0 = base + Cfg::kSlab + bi * slab, ysa = at0 + 1024, vsa = ysa + C * pv, usa = vsa + C * pv, ssa = usa + 2 * UB;
+        vec = reinterpret_cast<const float *>(buf);
+        if (h == 0 && part == 0) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) qk[r] = kk[r] = 0.f;
-      if (low) {
+          for (int u = 0; u < JT; ++u)
 #pragma unroll
-        for (int kt = 0; kt < K / 16; ++kt) {
-          uint32_t qa[4], ka[4], kb[2];
-          const uint32_t ra = (i0 + (lane & 15)) * Cfg::kPK + 32 * kt + 16 * mhi;
-          ldmatrix_x4(qsa + ra, qa);
-          ldmatrix_x4(ksa + ra, ka);
-          ldmatrix_x2(ksa + (8 * kq + mrow) * Cfg::kPK + 32 * kt + 16 * mlo, kb);
-          mma_bf16_16816(qk, qa, kb[0], kb[1]);
-          mma_bf16_16816(kk, ka, kb[0], kb[1]);
+            for (int r = 0; r < 4; ++r) qk[u][r] = kk[u][r] = 0.f;
+#pragma unroll
+          for (int kt = 0; kt < K / 16; ++kt) {
+            uint32_t qa[4], ka[4];
+            const uint32_t ra = (i0 + (lane & 15)) * Cfg::kPK + 32 * kt + 16 * mhi;
+            ldmatrix_x4(qsa + ra, qa);
+            ldmatrix_x4(ksa + ra, ka);
+#pragma unroll
+            for (int u = 0; u < JT; ++u)
+              if (JT * kq + u <= 2 * mh + 1) {
+                uint32_t kb[2];
+                ldmatrix_x2(ksa + (8 * (JT * kq + u) + mrow) * Cfg::kPK + 32 * kt + 16 * mlo, kb);
+                mma_bf16_16816(qk[u], qa, kb[0], kb[1]);
+                mma_bf16_16816(kk[u], ka, kb[0], kb[1]);
+              }
+          }
+        }
+        {      // <S, dS'>
+          const unsigned char *sp = buf + (ssa - at0);
+#pragma unroll
+          for (int x0 = 0; x0 < K * P; x0 += kThreads) {
+            const int x = x0 + tid;
+            if (K * P % kThreads && x >= K * P) break;
+            const uint4 p = *reinterpret_cast<const uint4 *>(sp + 16 * x), d = *reinterpret_cast<const uint4 *>(sp + SB + 16 * x);
+            ss = fma_bf16<0, 0>(p.x, d.x, fma_bf16<1, 1>(p.x, d.x, ss));
+            ss = fma_bf16<0, 0>(p.y, d.y, fma_bf16<1, 1>(p.y, d.y, ss));
+            ss = fma_bf16<0, 0>(p.z, d.z, fma_bf16<1, 1>(p.z, d.z, ss));
+            ss = fma_bf16<0, 0>(p.w, d.w, fma_bf16<1, 1>(p.w, d.w, ss));
+          }
+        }
+        // products over the slab's columns
+        const uint32_t y_at = ysa + (i0 + mrow + 8 * mlo) * pv + 16 * mhi, v_at = vsa + (8 * JT * kq + mrow) * pv + 16 * mlo;
+        const uint32_t b_at = usa + 16 * mrow + 128 * (4 * mhi + 2 * mh + mlo), u_at = usa + 16 * mrow + 128 * (4 * mlo + JT * kq);   // blocks [column tile][token tile]
+        const uint32_t s_one = ssa + 16 * mrow + 128 * (mlo * (K / 8) + f0 / 8), s_at = s_one + 128 * mhi;
+#pragma unroll
+        for (int kt = 0; kt < VS / 16; ++kt) {
+          uint32_t ya[4], la[4], ua[4];     // A operands: 16 tokens x 16 columns
+          ldmatrix_x4(y_at + 32 * kt, ya);
+          ldmatrix_x4_t(b_at + 1024 * kt, ua);
+          ldmatrix_x4_t(b_at + UB + 1024 * kt, la);
+#pragma unroll
+          for (int u = 0; u < JT; ++u)
+            if (JT * kq + u <= 2 * mh + 1) {
+              uint32_t ub[2];               // B operands: 16 columns x 8 tokens
+              ldmatrix_x2_t(u_at + 1024 * kt + 128 * u, ub);
+              mma_bf16_16816(yu[u], ya, ub[0], ub[1]);
+              mma_bf16_16816(lu[u], la, ub[0], ub[1]);
+              if (JT * kq + u >= 2 * mh) {
+                ldmatrix_x2(v_at + 32 * kt + 8 * u * pv, ub);
+                mma_bf16_16816(ld[u], la, ub[0], ub[1]);
+              }
+            }
+#pragma unroll
+          for (int t = 0; t < NT; t += 2) {
+            // B operands: 16 columns x 16 features (of a last tile alone the second is not used)
+            if (t >= tiles) continue;
+            const uint32_t at = (t + 1 < tiles ? s_at : s_one) + 32 * K * kt + 128 * t;
+            uint32_t sb[4], db[4];
+            ldmatrix_x4_t(at, sb);
+            ldmatrix_x4_t(at + SB, db);
+            mma_bf16_16816(dq[t], ya, sb[0], sb[1]);
+            mma_bf16_16816(dm[t], la, sb[0], sb[1]);
+            mma_bf16_16816(dp[t], ua, db[0], db[1]);
+            if (t + 1 < NT && t + 1 < tiles) {
+              mma_bf16_16816(dq[t + 1], ya, sb[2], sb[3]);
+              mma_bf16_16816(dm[t + 1], la, sb[2], sb[3]);
+              mma_bf16_16816(dp[t + 1], ua, db[2], db[3]);
+            }
+          }
+        }
+        if (BUFS == 1 && part + 1 < parts) {
+          __syncthreads();      // (the slab's place is the next one's)
+          fetch(o, n, part + 1, 0);
         }
       }
-    }
-    {      // <S, dS'>
-      const unsigned char *sp = buf + (ssa - at0);
+      // X1, X2; rows i of this thread: i0 + g, i0 + g + 8
+      float bt[2], r1[2] = {}, r2[2] = {};
 #pragma unroll
-      for (int x0 = 0; x0 < K * P; x0 += kThreads) {
-        const int x = x0 + tid;
-        if (K * P % kThreads && x >= K * P) break;
-        const uint4 p = *reinterpret_cast<const uint4 *>(sp + 16 * x), d = *reinterpret_cast<const uint4 *>(sp + SB + 16 * x);
-        ss = fma_bf16<0, 0>(p.x, d.x, fma_bf16<1, 1>(p.x, d.x, ss));
-        ss = fma_bf16<0, 0>(p.y, d.y, fma_bf16<1, 1>(p.y, d.y, ss));
-        ss = fma_bf16<0, 0>(p.z, d.z, fma_bf16<1, 1>(p.z, d.z, ss));
-        ss = fma_bf16<0, 0>(p.w, d.w, fma_bf16<1, 1>(p.w, d.w, ss));
-      }
-    }
-    // products over the slab's columns
-    const uint32_t y_at = ysa + (i0 + mrow + 8 * mlo) * pv + 16 * mhi, v_at = vsa + (8 * kq + mrow) * pv + 16 * mlo;
-    const uint32_t b_at = usa + 16 * mrow + 128 * (4 * mhi + 2 * mh + mlo), u_at = usa + 16 * mrow + 128 * (4 * mlo + kq);   // blocks [column tile][token tile]
-    const uint32_t s_at = ssa + 16 * mrow + 128 * (mlo * (K / 8) + f0 / 8 + mhi), s_one = ssa + 16 * mrow + 128 * (mlo * (K / 8) + f0 / 8);
+      for (int x = 0; x < 2; ++x) bt[x] = vec[32 * kVecBeta + i0 + g + 8 * x];
 #pragma unroll
-    for (int kt = 0; kt < VS / 16; ++kt) {
-      uint32_t ya[4], la[4], ua[4];     // A operands: 16 tokens x 16 columns
-      ldmatrix_x4(y_at + 32 * kt, ya);
-      ldmatrix_x4_t(b_at + 1024 * kt, ua);
-      ldmatrix_x4_t(b_at + UB + 1024 * kt, la);
-      if (low) {
-        uint32_t ub[2], wb[2];          // B operands: 16 columns x 8 tokens from 8 kq
-        ldmatrix_x2_t(u_at + 1024 * kt, ub);
-        mma_bf16_16816(yu, ya, ub[0], ub[1]);
-        mma_bf16_16816(lu, la, ub[0], ub[1]);
-        ldmatrix_x2(v_at + 32 * kt, wb);      // (needed on the diagonal alone)
-        mma_bf16_16816(ld, la, wb[0], wb[1]);
-      }
+      for (int u = 0; u < JT; ++u) {
+        const int jt = JT * kq + u, jj = 8 * jt + 2 * c;
+        if (jt > 2 * mh + 1) continue;
+        const float2 gj = *reinterpret_cast<const float2 *>(vec + 32 * kVecG + jj), rj = *reinterpret_cast<const float2 *>(vec + 32 * kVecRk + jj);
+        float c0 = 0.f, c1 = 0.f;
 #pragma unroll
-      for (int t = 0; t < NT; t += 2) {
-        // B operands: 16 columns x 16 features (of a last tile alone the second is not used)
-        if (t >= tiles) continue;
-        const uint32_t at = (t + 1 < tiles ? s_at : s_one) + 32 * K * kt + 128 * t;
-        uint32_t sb[4], db[4];
-        ldmatrix_x4_t(at, sb);
-        ldmatrix_x4_t(at + SB, db);
-        mma_bf16_16816(dq[t], ya, sb[0], sb[1]);
-        mma_bf16_16816(dm[t], la, sb[0], sb[1]);
-        mma_bf16_16816(dp[t], ua, db[0], db[1]);
-        if (t + 1 < NT && t + 1 < tiles) {
-          mma_bf16_16816(dq[t + 1], ya, sb[2], sb[3]);
-          mma_bf16_16816(dm[t + 1], la, sb[2], sb[3]);
-          mma_bf16_16816(dp[t + 1], ua, db[2], db[3]);
+        for (int x = 0; x < 2; ++x) {
+          const int i = i0 + g + 8 * x;
+          const float gi = vec[32 * kVecG + i], rk = vec[32 * kVecRk + i], rq = a.scale * vec[32 * kVecRq + i];
+          const float e0 = i >= jj ? __expf(gi - gj.x) * rj.x : 0.f, e1 = i > jj ? __expf(gi - gj.y) * rj.y : 0.f;
+          const float x10 = rq * e0 * yu[u][2 * x], x11 = rq * e1 * yu[u][2 * x + 1];
+          const float m0 = i > jj ? -rk * e0 * lu[u][2 * x] : 0.f, m1 = i > jj + 1 ? -rk * e1 * lu[u][2 * x + 1] : 0.f;
+          const float t0 = x10 * qk[u][2 * x], t1 = x11 * qk[u][2 * x + 1], u0 = m0 * kk[u][2 * x], u1 = m1 * kk[u][2 * x + 1];
+          c0 += fmaf(bt[x], u0, i > jj ? t0 : 0.f);
+          c1 += fmaf(bt[x], u1, i > jj + 1 ? t1 : 0.f);
+          if (i == jj) { red[32 * Cfg::kDiag + i] = t0; red[32 * Cfg::kLv + i] = ld[u][2 * x]; }
+          if (i == jj + 1) { red[32 * Cfg::kDiag + i] = t1; red[32 * Cfg::kLv + i] = ld[u][2 * x + 1]; }
+          r1[x] += t0 + t1;
+          r2[x] += u0 + u1;
+          x1s[u][2 * x] = x10 + (MULTI && h ? x1s[u][2 * x] : 0.f);
+          x1s[u][2 * x + 1] = x11 + (MULTI && h ? x1s[u][2 * x + 1] : 0.f);
+          x2s[u][2 * x] = fmaf(bt[x], m0, MULTI && h ? x2s[u][2 * x] : 0.f);
+          x2s[u][2 * x + 1] = fmaf(bt[x], m1, MULTI && h ? x2s[u][2 * x + 1] : 0.f);
         }
-      }
-    }
-    }
-    // rows i of this thread: i0 + g, i0 + g + 8
-    float bt[2], eq[2], egk[2], ek[2];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int i = i0 + g + 8 * x;
-      bt[x] = vec[32 * kVecBeta + i]; eq[x] = vec[32 * kVecEq + i]; egk[x] = vec[32 * kVecEgk + i]; ek[x] = vec[32 * kVecEk + i];
-    }
-    if (low) {
-      const int j = 8 * kq + 2 * c;
-      const float2 gj = *reinterpret_cast<const float2 *>(vec + 32 * kVecG + j), rj = *reinterpret_cast<const float2 *>(vec + 32 * kVecRk + j);
-      float c0 = 0.f, c1 = 0.f;
+        for (int d = 4; d < 32; d *= 2) {
+          c0 += __shfl_xor_sync(0xffffffffu, c0, d);
+          c1 += __shfl_xor_sync(0xffffffffu, c1, d);
+        }
+        if (g == 0) *reinterpret_cast<float2 *>(red + 32 * (Cfg::kCol + mh) + jj) = make_float2(c0, c1);
+      }
+      if (mh == 0 && JT * kq + JT > 2 && g == 0)      // (columns that the upper half of the rows does not reach)
+#pragma unroll
+        for (int u = 0; u < JT; ++u)
+          if (JT * kq + u >= 2) *reinterpret_cast<float2 *>(red + 32 * Cfg::kCol + 8 * (JT * kq + u) + 2 * c) = make_float2(0.f, 0.f);
+      // a1, a2, a3; the products with the states scaled and put together
+      float a1[2] = {}, a2[2] = {}, a3[2] = {};
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int i = i0 + g + 8 * x;
-        const float gi = vec[32 * kVecG + i], rk = vec[32 * kVecRk + i], rq = a.scale * vec[32 * kVecRq + i];
-        const float e0 = i >= j ? __expf(gi - gj.x) * rj.x : 0.f, e1 = i > j ? __expf(gi - gj.y) * rj.y : 0.f;
-        const float x10 = rq * e0 * yu[2 * x], x11 = rq * e1 * yu[2 * x + 1];
-        const float n0_ = i > j ? -rk * e0 * lu[2 * x] : 0.f, n1_ = i > j + 1 ? -rk * e1 * lu[2 * x + 1] : 0.f;
-        const uint32_t at = mat + 128 * (4 * (2 * mh + x) + kq) + 4 * lane;
-        sts32(at, __uint_as_float(pack_bf16(x10, x11)));
-        sts32(at + 2048, __uint_as_float(pack_bf16(bt[x] * n0_, bt[x] * n1_)));
-        const float t0 = x10 * qk[2 * x], t1 = x11 * qk[2 * x + 1], u0 = n0_ * kk[2 * x], u1 = n1_ * kk[2 * x + 1];
-        c0 += fmaf(bt[x], u0, i > j ? t0 : 0.f);
-        c1 += fmaf(bt[x], u1, i > j + 1 ? t1 : 0.f);
-        if (i == j) { red[32 * kDiag + i] = t0; red[32 * kLv + i] = ld[2 * x]; }
-        if (i == j + 1) { red[32 * kDiag + i] = t1; red[32 * kLv + i] = ld[2 * x + 1]; }
-        float r1 = t0 + t1, r2 = u0 + u1;
-        r1 += __shfl_xor_sync(0xffffffffu, r1, 1);
-        r2 += __shfl_xor_sync(0xffffffffu, r2, 1);
-        r1 += __shfl_xor_sync(0xffffffffu, r1, 2);
-        r2 += __shfl_xor_sync(0xffffffffu, r2, 2);
-        if (c == 0) { red[32 * (kRow1 + kq) + i] = r1; red[32 * (kRow2 + kq) + i] = r2; }
+        const float eq = vec[32 * kVecEq + i], be = -bt[x] * vec[32 * kVecEgk + i], ek = vec[32 * kVecEk + i];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          if (t >= tiles) continue;
+          const float2 qv = unpack_bf16(__float_as_uint(lds32(qat + 8 * x * Cfg::kPK + 16 * t))), kv = unpack_bf16(__float_as_uint(lds32(kat + 8 * x * Cfg::kPK + 16 * t)));
+          a1[x] = fmaf(qv.x, dq[t][2 * x], fmaf(qv.y, dq[t][2 * x + 1], a1[x]));
+          a2[x] = fmaf(kv.x, dm[t][2 * x], fmaf(kv.y, dm[t][2 * x + 1], a2[x]));
+          a3[x] = fmaf(kv.x, dp[t][2 * x], fmaf(kv.y, dp[t][2 * x + 1], a3[x]));
+#pragma unroll
+          for (int e = 2 * x; e < 2 * x + 2; ++e) {
+            dqs[t][e] = fmaf(eq, dq[t][e], MULTI && h ? dqs[t][e] : 0.f);
+            dks[t][e] = fmaf(be, dm[t][e], fmaf(ek, dp[t][e], MULTI && h ? dks[t][e] : 0.f));
+          }
+        }
+#pragma unroll
+        for (int d = 1; d < 4; d *= 2) {
+          a1[x] += __shfl_xor_sync(0xffffffffu, a1[x], d);
+          a2[x] += __shfl_xor_sync(0xffffffffu, a2[x], d);
+          a3[x] += __shfl_xor_sync(0xffffffffu, a3[x], d);
+          r1[x] += __shfl_xor_sync(0xffffffffu, r1[x], d);
+          r2[x] += __shfl_xor_sync(0xffffffffu, r2[x], d);
+        }
+        red[32 * (Cfg::kA + KG * c + kq) + i] = c == 0 ? a1[x] : c == 1 ? a2[x] : c == 2 ? a3[x] : r1[x];      // (kRow1 follows a3)
+        if (c == 0) red[32 * (Cfg::kRow2 + kq) + i] = r2[x];
       }
 #pragma unroll
-      for (int d = 4; d < 32; d *= 2) {
-        c0 += __shfl_xor_sync(0xffffffffu, c0, d);
-        c1 += __shfl_xor_sync(0xffffffffu, c1, d);
-      }
-      if (g == 0) *reinterpret_cast<float2 *>(red + 32 * (kCol + mh) + j) = make_float2(c0, c1);
-    } else {      // (16 mh, 8 kq) above the diagonal: nothing to add
-      if (c == 0) red[32 * (kRow1 + kq) + i0 + g] = red[32 * (kRow1 + kq) + i0 + g + 8] = red[32 * (kRow2 + kq) + i0 + g] = red[32 * (kRow2 + kq) + i0 + g + 8] = 0.f;
-      if (g == 0) *reinterpret_cast<float2 *>(red + 32 * (kCol + mh) + 8 * kq + 2 * c) = make_float2(0.f, 0.f);
-    }
-    // a1, a2, a3; the products with the states scaled and put together
-    uint32_t qw[NT][2], kw[NT][2];
-    float a1[2] = {}, a2[2] = {}, a3[2] = {};
+      for (int d = 16; d; d /= 2) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+      if (lane == 0) red[32 * Cfg::kSds + warp] = ss;
+      if (!MULTI || h + 1 == a.hpc) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+        for (int u = 0; u < JT; ++u) {
+          if (JT * kq + u > 2 * mh + 1) continue;
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        if (t >= tiles) continue;
-        qw[t][x] = __float_as_uint(lds32(qat + 8 * x * Cfg::kPK + 16 * t));
-        kw[t][x] = __float_as_uint(lds32(kat + 8 * x * Cfg::kPK + 16 * t));
-        const float2 qv = unpack_bf16(qw[t][x]), kv = unpack_bf16(kw[t][x]);
-        a1[x] = fmaf(qv.x, dq[t][2 * x], fmaf(qv.y, dq[t][2 * x + 1], a1[x]));
-        a2[x] = fmaf(kv.x, dm[t][2 * x], fmaf(kv.y, dm[t][2 * x + 1], a2[x]));
-        a3[x] = fmaf(kv.x, dp[t][2 * x], fmaf(kv.y, dp[t][2 * x + 1], a3[x]));
-        const float be = -bt[x] * egk[x];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          dq[t][2 * x + e] *= eq[x];
-          dm[t][2 * x + e] = fmaf(be, dm[t][2 * x + e], ek[x] * dp[t][2 * x + e]);
+          for (int x = 0; x < 2; ++x) {
+            const uint32_t at = mat + 128 * (4 * (2 * mh + x) + JT * kq + u) + 4 * lane;
+            sts32(at, __uint_as_float(pack_bf16(x1s[u][2 * x], x1s[u][2 * x + 1])));
+            sts32(at + 2048, __uint_as_float(pack_bf16(x2s[u][2 * x], x2s[u][2 * x + 1])));
+          }
         }
       }
+      __syncthreads();
+      if (warp == 0) {      // a token a lane
+        auto sum = [&](int r) {
+          const float *p = red + 32 * r + lane;
+          float s = p[0];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      a1[x] += __shfl_xor_sync(0xffffffffu, a1[x], 1);
-      a2[x] += __shfl_xor_sync(0xffffffffu, a2[x], 1);
-      a3[x] += __shfl_xor_sync(0xffffffffu, a3[x], 1);
-      a1[x] += __shfl_xor_sync(0xffffffffu, a1[x], 2);
-      a2[x] += __shfl_xor_sync(0xffffffffu, a2[x], 2);
-      a3[x] += __shfl_xor_sync(0xffffffffu, a3[x], 2);
-      if (c < 3) red[32 * (kA + 4 * c + kq) + i0 + g + 8 * x] = c == 0 ? a1[x] : c == 1 ? a2[x] : a3[x];
-    }
+          for (int x = 1; x < KG; ++x) s += p[32 * x];
+          return s;
+        };
+        const float b = vec[32 * kVecBeta + lane];
+        const float s1 = vec[32 * kVecEq + lane] * sum(Cfg::kA), s2 = vec[32 * kVecEgk + lane] * sum(Cfg::kA + KG), W = vec[32 * kVecEk + lane] * sum(Cfg::kA + 2 * KG);
+        const float r1 = sum(Cfg::kRow1), r2 = sum(Cfg::kRow2), col = red[32 * Cfg::kCol + lane] + red[32 * Cfg::kCol + 32 + lane], diag = red[32 * Cfg::kDiag + lane];
+        pqs = s1 + r1 + (MULTI && h ? pqs : 0.f);      // q . dq', k . dk'
+        pks = fmaf(b, r2 - s2, W + col + diag) + (MULTI && h ? pks : 0.f);
+        if (!MULTI || h + 1 == a.hpc) {
+          const float rk = vec[32 * kVecRk + lane], rq = vec[32 * kVecRq + lane];
+          red[32 * Cfg::kUq + lane] = a.qk_norm ? -rq * rq * pqs : 0.f;
+          red[32 * Cfg::kUk + lane] = a.qk_norm ? -rk * rk * pks : 0.f;
+        }
+        float all = W, part = s1 + (r1 - diag) + b * (r2 - s2) - W - col;
 #pragma unroll
-    for (int d = 16; d; d /= 2) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-    if (lane == 0) red[32 * kSds + warp] = ss;
-    __syncthreads();
-    if (warp == 0) {      // a token a lane
-      auto sum4 = [&](int r) { const float *p = red + 32 * r + lane; return (p[0] + p[32]) + (p[64] + p[96]); };
-      const float b = vec[32 * kVecBeta + lane], rk = vec[32 * kVecRk + lane], rq = vec[32 * kVecRq + lane];
-      const float s1 = vec[32 * kVecEq + lane] * sum4(kA), s2 = vec[32 * kVecEgk + lane] * sum4(kA + 4), W = vec[32 * kVecEk + lane] * sum4(kA + 8);
-      const float r1 = sum4(kRow1), r2 = sum4(kRow2), col = red[32 * kCol + lane] + red[32 * kCol + 32 + lane], diag = red[32 * kDiag + lane];
-      const float pq = s1 + r1, pk = fmaf(b, r2 - s2, W + col + diag);      // q . dq', k . dk'
-      red[32 * kUq + lane] = a.qk_norm ? -rq * rq * pq : 0.f;
-      red[32 * kUk + lane] = a.qk_norm ? -rk * rk * pk : 0.f;
-      float all = W, part = s1 + (r1 - diag) + b * (r2 - s2) - W - col;
+        for (int d = 16; d; d /= 2) all += __shfl_xor_sync(0xffffffffu, all, d);
 #pragma unroll
-      for (int d = 16; d; d /= 2) all += __shfl_xor_sync(0xffffffffu, all, d);
+        for (int d = 1; d < 32; d *= 2) {
+          const float t = __shfl_down_sync(0xffffffffu, part, d);
+          if (lane + d < 32) part += t;
+        }
+        if (lane < o.have) {
+          const size_t at = (size_t)(o.tok + lane) * a.N + n;
+          float sd = 0.f;
 #pragma unroll
-      for (int d = 1; d < 32; d *= 2) {
-        const float o = __shfl_down_sync(0xffffffffu, part, d);
-        if (lane + d < 32) part += o;
-      }
-      if (lane < o.have) {
-        const size_t at = (size_t)(o.tok + lane) * a.N + n;
-        const float4 p = *reinterpret_cast<const float4 *>(red + 32 * kSds), q = *reinterpret_cast<const float4 *>(red + 32 * kSds + 4);
-        const float dlog = part + all + expf(vec[32 * kVecG + 31]) * (((p.x + p.y) + (p.z + p.w)) + ((q.x + q.y) + (q.z + q.w)));
-        static_cast<__nv_bfloat16 *>(a.dgate)[at] = __float2bfloat16_rn(dlog * vec[32 * kVecDlog + lane]);
-        static_cast<__nv_bfloat16 *>(a.dstep)[at] = __float2bfloat16_rn((red[32 * kLv + lane] - s2 + r2) * (a.step_kind == M2RNN_STEP_LOGIT ? b * (1.f - b) : 1.f));
+          for (int x = 0; x < 2 * KG; ++x) sd += red[32 * Cfg::kSds + x];
+          const float dlog = fmaf(expf(vec[32 * kVecG + 31]), sd, part + all);
+          static_cast<__nv_bfloat16 *>(a.dgate)[at] = __float2bfloat16_rn(dlog * vec[32 * kVecDlog + lane]);
+          static_cast<__nv_bfloat16 *>(a.dstep)[at] = __float2bfloat16_rn((red[32 * Cfg::kLv + lane] - s2 + r2) * (a.step_kind == M2RNN_STEP_LOGIT ? b * (1.f - b) : 1.f));
+        }
       }
     }
 #pragma unroll
@@ -377,82 +391,88 @@ __global__ void __launch_bounds__(kThreads, 2) delta_grad_kernel(DeltaArgs a, un
       for (int t = 0; t < NT; t += 2) {
         if (t >= tiles) continue;
         const uint32_t at = (16 * kt + mrow + 8 * mlo) * Cfg::kPK + 2 * f0 + 16 * (t + (t + 1 < tiles ? mhi : 0));
-        uint32_t kb[4], qb[4];
+        uint32_t kb[4], qb4[4];
         ldmatrix_x4_t(ksa + at, kb);
-        if (up) ldmatrix_x4_t(qsa + at, qb);
+        if (up) ldmatrix_x4_t(qsa + at, qb4);
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-          if (t + e < NT) {
-            if (t + e >= tiles) continue;
+          if (t + e < NT && t + e < tiles) {
             if (lo) {
-              mma_bf16_16816(dq[t + e], x1, kb[2 * e], kb[2 * e + 1]);
-              mma_bf16_16816(dm[t + e], x2, kb[2 * e], kb[2 * e + 1]);
+              mma_bf16_16816(dqs[t + e], x1, kb[2 * e], kb[2 * e + 1]);
+              mma_bf16_16816(dks[t + e], x2, kb[2 * e], kb[2 * e + 1]);
             }
             if (up) {
-              mma_bf16_16816(dm[t + e], t1, qb[2 * e], qb[2 * e + 1]);
-              mma_bf16_16816(dm[t + e], t2, kb[2 * e], kb[2 * e + 1]);
+              mma_bf16_16816(dks[t + e], t1, qb4[2 * e], qb4[2 * e + 1]);
+              mma_bf16_16816(dks[t + e], t2, kb[2 * e], kb[2 * e + 1]);
             }
           }
       }
     }
-    __syncthreads();      // the factors are there; X1, X2 and (at the last head) q and k are read
+    __syncthreads();      // the factors are there; X1, X2, q and k are read
+    if (BUFS == 1 && next.have) fetch(next, next.n0, 0, 0);
+    // through the division by the lengths: to the shares, or to the places of q and k
+    auto emit = [&](const float (&x)[NT][4], uint32_t at, int factors, float *part) {
+      if (part) part += ((size_t)(o.tok + i0 + g) * a.shares + o.run) * K + f0 + 2 * c;
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const float uq = red[32 * kUq + i0 + g + 8 * x], uk = red[32 * kUk + i0 + g + 8 * x];
+      for (int y = 0; y < 2; ++y) {
+        const float f = red[32 * factors + i0 + g + 8 * y];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        if (t >= tiles) continue;
-        const float2 qv = unpack_bf16(qw[t][x]), kv = unpack_bf16(kw[t][x]);
-        dq[t][2 * x] = fmaf(uq, qv.x, dq[t][2 * x]);
-        dq[t][2 * x + 1] = fmaf(uq, qv.y, dq[t][2 * x + 1]);
-        dm[t][2 * x] = fmaf(uk, kv.x, dm[t][2 * x]);
-        dm[t][2 * x + 1] = fmaf(uk, kv.y, dm[t][2 * x + 1]);
-        if constexpr (MULTI)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            dqs[t][2 * x + e] += dq[t][2 * x + e];
-            dks[t][2 * x + e] += dm[t][2 * x + e];
-          }
+        for (int t = 0; t < NT; ++t) {
+          if (t >= tiles) continue;
+          const float2 was = unpack_bf16(__float_as_uint(lds32(at + 8 * y * Cfg::kPK + 16 * t)));
+          const float v0 = fmaf(f, was.x, x[t][2 * y]), v1 = fmaf(f, was.y, x[t][2 * y + 1]);
+          if (!part) sts32(at + 8 * y * Cfg::kPK + 16 * t, __uint_as_float(pack_bf16(v0, v1)));
+          else if (i0 + g + 8 * y < o.have) *reinterpret_cast<float2 *>(part + (size_t)8 * y * a.shares * K + 8 * t) = make_float2(v0, v1);
+        }
       }
+    };
+    emit(dqs, qat, Cfg::kUq, a.dq_part);
+    emit(dks, kat, Cfg::kUk, a.dk_part);
+    __syncthreads();
+    for (int x = tid; x < o.have * (K / 8); x += kThreads) {
+      const int r = x / (K / 8), p = x % (K / 8);
+      if (!a.dq_part) *reinterpret_cast<float4 *>(static_cast<__nv_bfloat16 *>(a.dq) + ((size_t)(o.tok + r) * a.Nq + o.hq) * K + 8 * p) = lds128(qsa + r * Cfg::kPK + 16 * p);
+      if (!a.dk_part) *reinterpret_cast<float4 *>(static_cast<__nv_bfloat16 *>(a.dk) + ((size_t)(o.tok + r) * a.Nk + o.hk) * K + 8 * p) = lds128(ksa + r * Cfg::kPK + 16 * p);
     }
-    if constexpr (!MULTI) emit(dq, dm);
-  }
-  if constexpr (MULTI) emit(dqs, dks);
-  __syncthreads();
-  for (int x = tid; x < o.have * (K / 8); x += kThreads) {
-    const int r = x / (K / 8), p = x % (K / 8);
-    if (!a.dq_part) *reinterpret_cast<float4 *>(static_cast<__nv_bfloat16 *>(a.dq) + ((size_t)(o.tok + r) * a.Nq + o.hq) * K + 8 * p) = lds128(qsa + r * Cfg::kPK + 16 * p);
-    if (!a.dk_part) *reinterpret_cast<float4 *>(static_cast<__nv_bfloat16 *>(a.dk) + ((size_t)(o.tok + r) * a.Nk + o.hk) * K + 8 * p) = lds128(ksa + r * Cfg::kPK + 16 * p);
-  }
-  if (!next.have) break;
-  o = next;
+    if (!next.have) break;
+    o = next;
   }
 }
 
 template <int K, bool MULTI, int VS> cudaError_t launch_kmv(const DeltaArgs &a, cudaStream_t s) {
-  constexpr size_t smem = GradCfg<K>::kSlab + 2 * (size_t)slab_bytes(K, VS);
-  static_assert(smem <= 113 * 1024, "two CTAs to an SM");
-  const cudaError_t e = allow_smem(delta_grad_kernel<K, MULTI, VS>, smem);
+  constexpr int KG = 2, CTAS = K > 64 ? 2 : 3;
+  using Cfg = GradCfg<K, KG>;
+  constexpr int room = 227 * 1024 / CTAS - 1024, BUFS = MULTI || Cfg::kSlab + 2 * slab_bytes(K, VS) <= room ? 2 : 1;
+  constexpr size_t smem = Cfg::kSlab + BUFS * (size_t)slab_bytes(K, VS);
+  static_assert(smem <= room, "CTAs to an SM");
+  const auto kernel = delta_grad_kernel<K, KG, MULTI, VS, BUFS, CTAS>;
+  const cudaError_t e = allow_smem(kernel, smem);
   if (e != cudaSuccess) return e;
-  const unsigned jobs = (unsigned)((long long)a.B * a.nch * (a.N / a.hpc)), most = 2 * (unsigned)sm_count();
-  return launch_early(delta_grad_kernel<K, MULTI, VS>, dim3(jobs < most ? jobs : most), dim3(kThreads), smem, s, a, jobs);
+  const unsigned jobs = (unsigned)((long long)a.B * a.nch * (a.N / a.hpc)), most = CTAS * (unsigned)sm_count();
+  return launch_early(kernel, dim3(jobs < most ? jobs : most), dim3(Cfg::kThreads), smem, s, a, jobs);
 }
 template <int K, bool MULTI> cudaError_t launch_km(const DeltaArgs &a, cudaStream_t s) {
+  constexpr int VS = MULTI || K > 64 ? 32 : 64;
   if (a.V == 16) return launch_kmv<K, MULTI, 16>(a, s);
-  if (a.V == 32 || GradCfg<K>::VS == 32) return launch_kmv<K, MULTI, 32>(a, s);
-  return launch_kmv<K, MULTI, GradCfg<K>::VS>(a, s);
+  if (a.V == 32 || VS == 32) return launch_kmv<K, MULTI, 32>(a, s);
+  return launch_kmv<K, MULTI, VS>(a, s);
 }
 template <int K> cudaError_t launch_k(const DeltaArgs &a, cudaStream_t s) { return a.hpc > 1 ? launch_km<K, true>(a, s) : launch_km<K, false>(a, s); }
 
 }  // namespace
 
-// Heads of a CTA: as many of those that share q and k as leave four CTAs for every SM
+// Heads of a job, of those that share q and k: the most that keep the CTAs (two to an SM) busy for as few heads one after
+// the other as there can be
 int delta_grad_heads(const m2rnn_delta_params *p, size_t slots) {
-  int run = p->N / p->Nq, o = p->N / p->Nk;
+  int run = p->N / p->Nq, o = p->N / p->Nk, best = 1;
   while (o) { const int t = run % o; run = o; o = t; }
-  for (int d = run; d > 1; --d)
-    if (run % d == 0 && slots * (p->N / d) >= (size_t)4 * sm_count()) return d;
-  return 1;
+  size_t least = ~(size_t)0;
+  for (int d = run; d >= 1; --d) {
+    if (run % d) continue;
+    const size_t ctas = (size_t)(p->K > 64 ? 2 : 3) * sm_count(), rounds = (slots * (p->N / d) + ctas - 1) / ctas * d;
+    if (rounds + rounds / 32 < least) { least = rounds; best = d; }      // (fewer heads only where that saves 3 %: more shares to add up)
+  }
+  return best;
 }
 
 cudaError_t launch_delta_grad(const DeltaArgs &a, cudaStream_t s) {
