@@ -186,8 +186,8 @@ __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, 
               if (JT * kq + u <= 2 * mh + 1) {
                 uint32_t kb[2];
                 ldmatrix_x2(ksa + (8 * (JT * kq + u) + mrow) * Cfg::kPK + 32 * kt + 16 * mlo, kb);
-                mma_bf16_16816(qk[u], qa, kb[0], kb[1]);
-                mma_bf16_16816(kk[u], ka, kb[0], kb[1]);
+                mma_add(qk[u], qa, kb[0], kb[1]);
+                mma_add(kk[u], ka, kb[0], kb[1]);
               }
           }
         }
@@ -219,11 +219,11 @@ __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, 
             if (JT * kq + u <= 2 * mh + 1) {
               uint32_t ub[2];               // B operands: 16 columns x 8 tokens
               ldmatrix_x2_t(u_at + 1024 * kt + 128 * u, ub);
-              mma_bf16_16816(yu[u], ya, ub[0], ub[1]);
-              mma_bf16_16816(lu[u], la, ub[0], ub[1]);
+              mma_add(yu[u], ya, ub[0], ub[1]);
+              mma_add(lu[u], la, ub[0], ub[1]);
               if (JT * kq + u >= 2 * mh) {
                 ldmatrix_x2(v_at + 32 * kt + 8 * u * pv, ub);
-                mma_bf16_16816(ld[u], la, ub[0], ub[1]);
+                mma_add(ld[u], la, ub[0], ub[1]);
               }
             }
 #pragma unroll
@@ -234,13 +234,13 @@ __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, 
             uint32_t sb[4], db[4];
             ldmatrix_x4_t(at, sb);
             ldmatrix_x4_t(at + SB, db);
-            mma_bf16_16816(dq[t], ya, sb[0], sb[1]);
-            mma_bf16_16816(dm[t], la, sb[0], sb[1]);
-            mma_bf16_16816(dp[t], ua, db[0], db[1]);
+            mma_add(dq[t], ya, sb[0], sb[1]);
+            mma_add(dm[t], la, sb[0], sb[1]);
+            mma_add(dp[t], ua, db[0], db[1]);
             if (t + 1 < NT && t + 1 < tiles) {
-              mma_bf16_16816(dq[t + 1], ya, sb[2], sb[3]);
-              mma_bf16_16816(dm[t + 1], la, sb[2], sb[3]);
-              mma_bf16_16816(dp[t + 1], ua, db[2], db[3]);
+              mma_add(dq[t + 1], ya, sb[2], sb[3]);
+              mma_add(dm[t + 1], la, sb[2], sb[3]);
+              mma_add(dp[t + 1], ua, db[2], db[3]);
             }
           }
         }
@@ -398,12 +398,12 @@ __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, 
         for (int e = 0; e < 2; ++e)
           if (t + e < NT && t + e < tiles) {
             if (lo) {
-              mma_bf16_16816(dqs[t + e], x1, kb[2 * e], kb[2 * e + 1]);
-              mma_bf16_16816(dks[t + e], x2, kb[2 * e], kb[2 * e + 1]);
+              mma_add(dqs[t + e], x1, kb[2 * e], kb[2 * e + 1]);
+              mma_add(dks[t + e], x2, kb[2 * e], kb[2 * e + 1]);
             }
             if (up) {
-              mma_bf16_16816(dks[t + e], t1, qb4[2 * e], qb4[2 * e + 1]);
-              mma_bf16_16816(dks[t + e], t2, kb[2 * e], kb[2 * e + 1]);
+              mma_add(dks[t + e], t1, qb4[2 * e], qb4[2 * e + 1]);
+              mma_add(dks[t + e], t2, kb[2 * e], kb[2 * e + 1]);
             }
           }
       }

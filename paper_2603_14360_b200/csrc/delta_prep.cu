@@ -87,18 +87,18 @@ __global__ void __launch_bounds__(32 * kWarps) delta_prep_kernel(DeltaArgs a, in
     ldmatrix_x4(qsa + ra + 16 * Cfg::kPitch, q1);
     ldmatrix_x4(ksa + rb, b0);
     ldmatrix_x4(ksa + rb + 16 * Cfg::kPitch, b1);
-    mma_bf16_16816(kk[0], a0, b0[0], b0[1]);
-    mma_bf16_16816(kk[1], a0, b0[2], b0[3]);
-    mma_bf16_16816(kk[2], a1, b0[0], b0[1]);
-    mma_bf16_16816(kk[3], a1, b0[2], b0[3]);
-    mma_bf16_16816(kk[4], a1, b1[0], b1[1]);
-    mma_bf16_16816(kk[5], a1, b1[2], b1[3]);
-    mma_bf16_16816(qk[0], q0, b0[0], b0[1]);
-    mma_bf16_16816(qk[1], q0, b0[2], b0[3]);
-    mma_bf16_16816(qk[2], q1, b0[0], b0[1]);
-    mma_bf16_16816(qk[3], q1, b0[2], b0[3]);
-    mma_bf16_16816(qk[4], q1, b1[0], b1[1]);
-    mma_bf16_16816(qk[5], q1, b1[2], b1[3]);
+    mma_add(kk[0], a0, b0[0], b0[1]);
+    mma_add(kk[1], a0, b0[2], b0[3]);
+    mma_add(kk[2], a1, b0[0], b0[1]);
+    mma_add(kk[3], a1, b0[2], b0[3]);
+    mma_add(kk[4], a1, b1[0], b1[1]);
+    mma_add(kk[5], a1, b1[2], b1[3]);
+    mma_add(qk[0], q0, b0[0], b0[1]);
+    mma_add(qk[1], q0, b0[2], b0[3]);
+    mma_add(qk[2], q1, b0[0], b0[1]);
+    mma_add(qk[3], q1, b0[2], b0[3]);
+    mma_add(qk[4], q1, b1[0], b1[1]);
+    mma_add(qk[5], q1, b1[2], b1[3]);
   }
   __syncwarp();   // the tiles are read: their place is M's now
   // the factors that no head changes
