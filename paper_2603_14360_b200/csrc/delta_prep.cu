@@ -6,123 +6,134 @@
 // Differences g_i - g_j are formed before the exponential: no e^-g that could overflow.
 //
 // A warp does a chunk for all heads that share its q and k: the two products of 32 x 32 are taken once (mma.sync, fp32
-// accumulators that stay in registers), then for each head the gates, M, its inverse and P.  T is inverted in fp32:
+// accumulators that stay in registers), then for each head the gates, M, its inverse and P.  q and k go from memory
+// straight into operands: a lane of an operand's row takes eight neighbouring features (16 bytes) for four k slots; which
+// slot a feature has does not matter as long as both operands agree, and a row's words are the same as row of A
+// and as column of B.  T is inverted in fp32:
 // the two 16 x 16 blocks on the diagonal by forward substitution, a column a lane (a series of powers of M would
-// cancel digits where keys point the same way), then T_21 = -T_22 M_21 T_11.
+// cancel digits where keys point the same way), then T_21 = -(T_22 M_21) T_11 with tf32 operands (2^-12 of each, before T is rounded to bf16).
+// (With q and k through shared memory, ldmatrix and the last product in FMA: 361 us against 205 for 65 536 tokens of 32 heads, K = 128.)
 #include "delta_common.cuh"
 
 namespace m2rnn {
 namespace {
 
-constexpr int kWarps = 4, kPM = 36;   // pitch of M (floats)
+constexpr int kWarps = 4, kPM = 36, kPT = 20;   // pitches (floats) of M and of the diagonal blocks of T
+constexpr int kTHalf = 16 * kPT + 16;           // the second block, half the banks on
+constexpr int kWarpFloats = 32 * kPM + 2 * kTHalf;
 
-template <int K> struct PrepCfg {
-  static constexpr int kPitch = 2 * K + 16;                     // bytes; an odd number of 16: ldmatrix without conflicts
-  static constexpr int kTile = 32 * kPitch;
-  static constexpr int kScratch = (32 + 16) * kPM * 4 + 2048;   // M, T_22; then T as blocks (over the tiles, dead by then)
-  static constexpr int kWarpBytes = 2 * kTile > kScratch ? 2 * kTile : kScratch;
-};
+__device__ __forceinline__ uint32_t tf32(float x) {
+  uint32_t r;
+  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
 
 template <int K>
-__global__ void __launch_bounds__(32 * kWarps) delta_prep_kernel(DeltaArgs a, int run) {
-  using Cfg = PrepCfg<K>;
-  extern __shared__ __align__(128) unsigned char smem[];
+__global__ void __launch_bounds__(32 * kWarps, 4) delta_prep_kernel(DeltaArgs a, int run) {
+  __shared__ __align__(16) float sm[kWarps][kWarpFloats];
   begin_dependent();
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-  const int runs = a.N / run;
-  // (a packed batch's sequences are of different lengths: blocks of chunks that a sequence does not have leave at once)
-  const long long job = (long long)blockIdx.x * kWarps + warp;
-  const long long bc = job / runs;
-  const int n0 = (int)(job % runs) * run;
-  const int b = (int)(bc / a.nch), ch = (int)(bc % a.nch);
+  // (a packed batch's sequences are of different lengths: warps of chunks that a sequence does not have leave at once)
+  const unsigned runs = (unsigned)(a.N / run), job = blockIdx.x * kWarps + warp, bc = job / runs;
+  const int n0 = (int)(job - bc * runs) * run;
+  const int b = (int)(bc / (unsigned)a.nch), ch = (int)(bc - (unsigned)b * a.nch);
   if (b >= a.B) return;
   const DeltaSpan sp = delta_span<kDeltaChunk>(a, b);
   if (ch >= sp.n) return;
   const long long tok = sp.tok0 + ch * kDeltaChunk;
   const int have = min(kDeltaChunk, sp.T - ch * kDeltaChunk);
-  const int hq = n0 / (a.N / a.Nq), hk = n0 / (a.N / a.Nk);
+  const char *kg = static_cast<const char *>(a.k) + 2 * ((tok + g) * a.ks + (unsigned)n0 / (unsigned)a.per_k * K);
+  const char *qg = static_cast<const char *>(a.q) + 2 * ((tok + g) * a.qs + (unsigned)n0 / (unsigned)a.per_q * K);
+  const long long k8 = 16 * a.ks, q8 = 16 * a.qs;      // bytes to a row eight tokens on
 
-  unsigned char *mine = smem + warp * Cfg::kWarpBytes;
-  const uint32_t ksa = smem_u32(mine), qsa = ksa + Cfg::kTile;
-  {
-    const __nv_bfloat16 *kg = static_cast<const __nv_bfloat16 *>(a.k) + tok * a.ks + (long long)hk * K;
-    const __nv_bfloat16 *qg = static_cast<const __nv_bfloat16 *>(a.q) + tok * a.qs + (long long)hq * K;
-    for (int x = lane; x < 32 * (K / 8); x += 32) {
-      const int r = x / (K / 8), o = x % (K / 8);
-      const bool ok = r < have;
-      cp16_or_zero(ksa + r * Cfg::kPitch + 16 * o, kg + (ok ? r * a.ks : 0) + 8 * o, ok);
-      cp16_or_zero(qsa + r * Cfg::kPitch + 16 * o, qg + (ok ? r * a.qs : 0) + 8 * o, ok);
-    }
-    cp_wait_all();
-    __syncwarp();
-  }
-  // reciprocal lengths of this lane's token's rows
-  float rk = 1.f, rq = 1.f;
-  if (a.qk_norm) {
-    float sk = 0.f, sq = 0.f;
-    for (int o = 0; o < K / 8; ++o) {
-      const uint4 x = *reinterpret_cast<const uint4 *>(mine + lane * Cfg::kPitch + 16 * o);
-      const uint4 z = *reinterpret_cast<const uint4 *>(mine + Cfg::kTile + lane * Cfg::kPitch + 16 * o);
-      const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, zs[4] = {z.x, z.y, z.z, z.w};
+  // a head's gate and step entries (this lane's token's), asked for a head ahead
+  float gate_in = 0.f, step_in = 0.f, alpha = 1.f, beta = 0.f;
+  const bool mine = lane < have, psi = a.gate_kind == M2RNN_GATE_PSI;
+  auto gates = [&](int n) {
+    if (!mine) return;
+    const size_t at = (size_t)(tok + lane) * a.N + n;
+    gate_in = __bfloat162float(static_cast<const __nv_bfloat16 *>(a.gate)[at]);
+    step_in = __bfloat162float(static_cast<const __nv_bfloat16 *>(a.step)[at]);
+    if (psi) { alpha = a.alpha[n]; beta = a.beta[n]; }
+  };
+  gates(n0);
+  // the rows' 64-byte parts on their way to the L2, one a lane, while the first is waited for
+  if (64 * c < 2 * K && K > 32)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 u = unpack_bf16(xs[i]), w = unpack_bf16(zs[i]);
-        sk = fmaf(u.x, u.x, fmaf(u.y, u.y, sk));
-        sq = fmaf(w.x, w.x, fmaf(w.y, w.y, sq));
+    for (int x = 0; x < 4; ++x)
+      if (8 * x + g < have) {
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(kg + x * k8 + 64 * c));
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(qg + x * q8 + 64 * c));
+      }
+  // k k^T and q k^T, tiles (mt, nt) of 16 x 8 on and below the diagonal: mt = 0: nt 0, 1; mt = 1: nt 0 .. 3; of q q^T
+  // those on the diagonal
+  float kk[6][4] = {}, qk[6][4] = {}, qq[4][4] = {};
+  auto half = [&](const uint32_t (&k0)[4], const uint32_t (&k1)[4], const uint32_t (&q0)[4], const uint32_t (&q1)[4]) {      // 16 features: two words of each row
+    const uint32_t A0[4] = {k0[0], k0[1], k1[0], k1[1]}, A1[4] = {k0[2], k0[3], k1[2], k1[3]}, Q0[4] = {q0[0], q0[1], q1[0], q1[1]}, Q1[4] = {q0[2], q0[3], q1[2], q1[3]};
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) { mma_add(kk[nt], A0, k0[nt], k1[nt]); mma_add(qk[nt], Q0, k0[nt], k1[nt]); mma_add(qq[nt], Q0, q0[nt], q1[nt]); mma_add(qq[2 + nt], Q1, q0[2 + nt], q1[2 + nt]); }
+#pragma unroll
+    for (int nt = 0; nt < 4; ++nt) { mma_add(kk[2 + nt], A1, k0[nt], k1[nt]); mma_add(qk[2 + nt], Q1, k0[nt], k1[nt]); }
+  };
+#pragma unroll
+  for (int f = 0; f + 32 <= K; f += 32) {
+    uint4 kx[4], qx[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      kx[x] = qx[x] = make_uint4(0u, 0u, 0u, 0u);
+      if (8 * x + g < have) {
+        kx[x] = *reinterpret_cast<const uint4 *>(kg + x * k8 + 2 * f + 16 * c);
+        qx[x] = *reinterpret_cast<const uint4 *>(qg + x * q8 + 2 * f + 16 * c);
       }
     }
-    rk = 1.f / sqrtf(sk + a.eps);
-    rq = 1.f / sqrtf(sq + a.eps);
+    half({kx[0].x, kx[1].x, kx[2].x, kx[3].x}, {kx[0].y, kx[1].y, kx[2].y, kx[3].y}, {qx[0].x, qx[1].x, qx[2].x, qx[3].x}, {qx[0].y, qx[1].y, qx[2].y, qx[3].y});
+    half({kx[0].z, kx[1].z, kx[2].z, kx[3].z}, {kx[0].w, kx[1].w, kx[2].w, kx[3].w}, {qx[0].z, qx[1].z, qx[2].z, qx[3].z}, {qx[0].w, qx[1].w, qx[2].w, qx[3].w});
   }
-  // k k^T and q k^T, tiles (mt, nt) of 16 x 8 on and below the diagonal: mt = 0: nt 0, 1; mt = 1: nt 0 .. 3
-  float kk[6][4] = {}, qk[6][4] = {};
+  if constexpr (K % 32) {
+    uint2 kx[4], qx[4];
 #pragma unroll
-  for (int kt = 0; kt < K / 16; ++kt) {
-    const uint32_t ra = (uint32_t)((lane & 15) * Cfg::kPitch + 32 * kt + 16 * (lane >> 4));                                 // A: rows lane % 16
-    const uint32_t rb = (uint32_t)(((lane & 7) + 8 * (lane >> 4)) * Cfg::kPitch + 32 * kt + 16 * ((lane >> 3) & 1));      // B: two tiles of tokens
-    uint32_t a0[4], a1[4], q0[4], q1[4], b0[4], b1[4];
-    ldmatrix_x4(ksa + ra, a0);
-    ldmatrix_x4(ksa + ra + 16 * Cfg::kPitch, a1);
-    ldmatrix_x4(qsa + ra, q0);
-    ldmatrix_x4(qsa + ra + 16 * Cfg::kPitch, q1);
-    ldmatrix_x4(ksa + rb, b0);
-    ldmatrix_x4(ksa + rb + 16 * Cfg::kPitch, b1);
-    mma_add(kk[0], a0, b0[0], b0[1]);
-    mma_add(kk[1], a0, b0[2], b0[3]);
-    mma_add(kk[2], a1, b0[0], b0[1]);
-    mma_add(kk[3], a1, b0[2], b0[3]);
-    mma_add(kk[4], a1, b1[0], b1[1]);
-    mma_add(kk[5], a1, b1[2], b1[3]);
-    mma_add(qk[0], q0, b0[0], b0[1]);
-    mma_add(qk[1], q0, b0[2], b0[3]);
-    mma_add(qk[2], q1, b0[0], b0[1]);
-    mma_add(qk[3], q1, b0[2], b0[3]);
-    mma_add(qk[4], q1, b1[0], b1[1]);
-    mma_add(qk[5], q1, b1[2], b1[3]);
+    for (int x = 0; x < 4; ++x) {
+      kx[x] = qx[x] = make_uint2(0u, 0u);
+      if (8 * x + g < have) {
+        kx[x] = *reinterpret_cast<const uint2 *>(kg + x * k8 + 2 * (K - 16) + 8 * c);
+        qx[x] = *reinterpret_cast<const uint2 *>(qg + x * q8 + 2 * (K - 16) + 8 * c);
+      }
+    }
+    half({kx[0].x, kx[1].x, kx[2].x, kx[3].x}, {kx[0].y, kx[1].y, kx[2].y, kx[3].y}, {qx[0].x, qx[1].x, qx[2].x, qx[3].x}, {qx[0].y, qx[1].y, qx[2].y, qx[3].y});
   }
-  __syncwarp();   // the tiles are read: their place is M's now
-  // the factors that no head changes
-  float rkj[4][2], rki[4], rqi[4];
+  // reciprocal lengths: of rows 8 x + g, of columns 8 x + 2c, + 1, and of this lane's token
+  float rki[4], rqi[4], rkj[4][2], rk = 1.f, rq = 1.f;
 #pragma unroll
   for (int x = 0; x < 4; ++x) {
-    rki[x] = __shfl_sync(0xffffffffu, rk, g + 8 * x);
-    rqi[x] = a.scale * __shfl_sync(0xffffffffu, rq, g + 8 * x);
-    rkj[x][0] = __shfl_sync(0xffffffffu, rk, 8 * x + 2 * c);
-    rkj[x][1] = __shfl_sync(0xffffffffu, rk, 8 * x + 2 * c + 1);
+    rki[x] = rqi[x] = 1.f;
+    if (a.qk_norm) {      // entry (g, g) of the diagonal's tile x is lane (g, g / 2)'s
+      const int tile = x < 2 ? x : 2 + x, r = 2 * (x & 1);
+      const float sk = __shfl_sync(0xffffffffu, g & 1 ? kk[tile][r + 1] : kk[tile][r], 4 * g + (g >> 1));
+      const float sq = __shfl_sync(0xffffffffu, g & 1 ? qq[x][r + 1] : qq[x][r], 4 * g + (g >> 1));
+      rki[x] = rsqrtf(sk + a.eps);
+      rqi[x] = rsqrtf(sq + a.eps);
+    }
+    rkj[x][0] = __shfl_sync(0xffffffffu, rki[x], 8 * c);
+    rkj[x][1] = __shfl_sync(0xffffffffu, rki[x], 8 * c + 4);
+    const float tk = __shfl_sync(0xffffffffu, rki[x], 4 * (lane & 7)), tq = __shfl_sync(0xffffffffu, rqi[x], 4 * (lane & 7));
+    if (lane >> 3 == x) { rk = tk; rq = tq; }
+    rqi[x] *= a.scale;
   }
-  float *M = reinterpret_cast<float *>(mine), *T22 = M + 32 * kPM;
-  unsigned char *Tb = reinterpret_cast<unsigned char *>(T22 + 16 * kPM);
+  float *M = sm[warp], *Td = M + 32 * kPM, *T22 = Td + kTHalf;
   const uint32_t Msa = smem_u32(M);
 
   for (int n = n0; n < n0 + run; ++n) {
     float la = 0.f, bt = 0.f, dlog = 0.f;
-    if (lane < have) {
-      const size_t at = (size_t)(tok + lane) * a.N + n;
-      const bool psi = a.gate_kind == M2RNN_GATE_PSI;
+    if (mine) {
       float unused;
-      la = delta_log_decay(a.gate_kind, __bfloat162float(static_cast<const __nv_bfloat16 *>(a.gate)[at]), psi ? a.alpha[n] : 1.f, psi ? a.beta[n] : 0.f, dlog);
-      bt = delta_step_of(a.step_kind, __bfloat162float(static_cast<const __nv_bfloat16 *>(a.step)[at]), unused);
+      la = delta_log_decay(a.gate_kind, gate_in, alpha, beta, dlog);
+      bt = delta_step_of(a.step_kind, step_in, unused);
     }
+    if (n + 1 < n0 + run) gates(n + 1);
     float gs = la;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
@@ -150,6 +161,7 @@ __global__ void __launch_bounds__(32 * kWarps) delta_prep_kernel(DeltaArgs a, in
       gi[x] = __shfl_sync(0xffffffffu, gs, g + 8 * x);
       bi[x] = __shfl_sync(0xffffffffu, bt, g + 8 * x) * rki[x];
     }
+    uint32_t *Pg = reinterpret_cast<uint32_t *>(rec + kRecP) + lane;
 #pragma unroll
     for (int nt = 0; nt < 4; ++nt) {
       const float g0 = __shfl_sync(0xffffffffu, gs, 8 * nt + 2 * c), g1 = __shfl_sync(0xffffffffu, gs, 8 * nt + 2 * c + 1);
@@ -159,20 +171,20 @@ __global__ void __launch_bounds__(32 * kWarps) delta_prep_kernel(DeltaArgs a, in
         const int tile = mt ? 2 + nt : nt;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int x = 2 * mt + h, i = g + 8 * x;
-          const float e0 = i >= j ? __expf(gi[x] - g0) * rkj[nt][0] : 0.f, e1 = i >= j + 1 ? __expf(gi[x] - g1) * rkj[nt][1] : 0.f;
-          const float m0 = i > j ? bi[x] * e0 * kk[tile][2 * h] : 0.f, m1 = i > j + 1 ? bi[x] * e1 * kk[tile][2 * h + 1] : 0.f;
+          const int x = 2 * mt + h, i = g + 8 * x;      // (blocks below the diagonal are whole, those above it nothing)
+          const bool w0 = x > nt || (x == nt && i >= j), w1 = x > nt || (x == nt && i > j);
+          const float e0 = w0 ? __expf(gi[x] - g0) * rkj[nt][0] : 0.f, e1 = w1 ? __expf(gi[x] - g1) * rkj[nt][1] : 0.f;
+          const float m0 = x > nt || i > j ? bi[x] * e0 * kk[tile][2 * h] : 0.f, m1 = x > nt || i > j + 1 ? bi[x] * e1 * kk[tile][2 * h + 1] : 0.f;
           sts64(Msa + 4u * (i * kPM + j), make_float2(m0, m1));
-          const float p0 = i >= j ? rqi[x] * e0 * qk[tile][2 * h] : 0.f, p1 = i >= j + 1 ? rqi[x] * e1 * qk[tile][2 * h + 1] : 0.f;
-          reinterpret_cast<uint32_t *>(rec + kRecP)[(4 * x + nt) * 32 + lane] = pack_bf16(p0, p1);
+          Pg[(4 * x + nt) * 32] = pack_bf16(rqi[x] * e0 * qk[tile][2 * h], rqi[x] * e1 * qk[tile][2 * h + 1]);
         }
       }
     }
     __syncwarp();
     // the diagonal blocks: lane (half, j) has column j of block `half`
-    const int half = lane >> 4, j = lane & 15;
-    float t[16];
     {
+      const int half = lane >> 4, j = lane & 15;
+      float t[16];
       const float *Mb = M + half * (16 * kPM + 16);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -186,79 +198,44 @@ __global__ void __launch_bounds__(32 * kWarps) delta_prep_kernel(DeltaArgs a, in
           if (m4 + 3 < i) s1 = fmaf(-w.w, t[m4 + 3], s1);
         }
         t[i] = s0 + s1;
-      }
-    }
-    if (half) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) T22[i * kPM + j] = t[i];
-    }
-    __nv_bfloat16 *tb = reinterpret_cast<__nv_bfloat16 *>(Tb);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) tb[(4 * (2 * half + (i >> 3)) + 2 * half + (j >> 3)) * 64 + (i & 7) * 8 + (j & 7)] = __float2bfloat16_rn(t[i]);
-    // Z = M_21 T_11: lane (half, j) rows 8 half .. of column j
-    float z[8];
-    {
-      float c11[16];
-#pragma unroll
-      for (int m = 0; m < 16; ++m) c11[m] = __shfl_sync(0xffffffffu, t[m], j);
-      const float *Mz = M + (16 + 8 * half) * kPM;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float s0 = 0.f, s1 = 0.f;
-#pragma unroll
-        for (int m4 = 0; m4 < 16; m4 += 4) {
-          const float4 w = *reinterpret_cast<const float4 *>(Mz + i * kPM + m4);
-          s0 = fmaf(w.x, c11[m4], s0);
-          s1 = fmaf(w.y, c11[m4 + 1], s1);
-          s0 = fmaf(w.z, c11[m4 + 2], s0);
-          s1 = fmaf(w.w, c11[m4 + 3], s1);
-        }
-        z[i] = s0 + s1;
+        Td[half * kTHalf + i * kPT + j] = t[i];
       }
     }
     __syncwarp();
-    {
-      float zz[16];
+    uint32_t *Tg = reinterpret_cast<uint32_t *>(rec + kRecT) + lane;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float o = __shfl_xor_sync(0xffffffffu, z[i], 16);
-        zz[i] = half ? o : z[i];
-        zz[8 + i] = half ? z[i] : o;
+    for (int d = 0; d < 2; ++d)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const float2 t = *reinterpret_cast<const float2 *>(Td + d * kTHalf + (8 * (x >> 1) + g) * kPT + 8 * (x & 1) + 2 * c);
+        Tg[(4 * (2 * d + (x >> 1)) + 2 * d + (x & 1)) * 32] = pack_bf16(t.x, t.y);
       }
-      const float *Tz = T22 + 8 * half * kPM;
+    // W = T_22 M_21; its accumulators are the next product's A operand with columns 2c, 2c + 1 in k slots c, c + 4
+    float W[2][4] = {}, Z[2][4] = {};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float s0 = 0.f, s1 = 0.f;
+    for (int kt = 0; kt < 2; ++kt) {
+      const float *t = T22 + g * kPT + 8 * kt + c, *m = M + (16 + 8 * kt + c) * kPM + g;
+      const uint32_t A[4] = {tf32(t[0]), tf32(t[8 * kPT]), tf32(t[4]), tf32(t[8 * kPT + 4])};
 #pragma unroll
-        for (int m4 = 0; m4 < 16; m4 += 4) {
-          const float4 w = *reinterpret_cast<const float4 *>(Tz + i * kPM + m4);
-          s0 = fmaf(w.x, zz[m4], s0);
-          s1 = fmaf(w.y, zz[m4 + 1], s1);
-          s0 = fmaf(w.z, zz[m4 + 2], s0);
-          s1 = fmaf(w.w, zz[m4 + 3], s1);
-        }
-        tb[(4 * (2 + half) + (j >> 3)) * 64 + i * 8 + (j & 7)] = __float2bfloat16_rn(-(s0 + s1));
-      }
+      for (int nt = 0; nt < 2; ++nt) mma_tf32(W[nt], A, tf32(m[8 * nt]), tf32(m[4 * kPM + 8 * nt]));
     }
-    __syncwarp();
-    {
-      // blocks 0, 1, 4, 5 and 8 .. 15
-      uint4 *out = reinterpret_cast<uint4 *>(rec + kRecT);
-      const uint4 *in = reinterpret_cast<const uint4 *>(Tb);
-      const int first = (lane & 7) + 8 * ((lane >> 3) & 1) + 32 * (lane >> 4);
-      out[first] = in[first];
-      out[64 + lane] = in[64 + lane];
-      out[96 + lane] = in[96 + lane];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      const float *t = Td + (8 * kt + 2 * c) * kPT + g;
+      const uint32_t A[4] = {tf32(-W[kt][0]), tf32(-W[kt][2]), tf32(-W[kt][1]), tf32(-W[kt][3])};
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) mma_tf32(Z[nt], A, tf32(t[8 * nt]), tf32(t[kPT + 8 * nt]));
+    }
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      Tg[(4 * 2 + nt) * 32] = pack_bf16(Z[nt][0], Z[nt][1]);
+      Tg[(4 * 3 + nt) * 32] = pack_bf16(Z[nt][2], Z[nt][3]);
     }
     __syncwarp();
   }
 }
 
 template <int K> cudaError_t launch_k(const DeltaArgs &a, cudaStream_t s) {
-  using Cfg = PrepCfg<K>;
-  constexpr size_t smem = (size_t)kWarps * Cfg::kWarpBytes;
-  cudaError_t e = allow_smem(delta_prep_kernel<K>, smem);
-  if (e != cudaSuccess) return e;
   const int dq = a.N / a.Nq, dk = a.N / a.Nk;
   int run = dq, o = dk;
   while (o) { const int t = run % o; run = o; o = t; }          // heads in a row that share both q and k
@@ -271,7 +248,7 @@ template <int K> cudaError_t launch_k(const DeltaArgs &a, cudaStream_t s) {
       if (chunks * (a.N / d) >= want) break;
     }
   const long long jobs = (long long)a.B * a.nch * (a.N / per);
-  return launch_early(delta_prep_kernel<K>, dim3((unsigned)((jobs + kWarps - 1) / kWarps)), dim3(32 * kWarps), smem, s, a, per);
+  return launch_early(delta_prep_kernel<K>, dim3((unsigned)((jobs + kWarps - 1) / kWarps)), dim3(32 * kWarps), 0, s, a, per);
 }
 
 }  // namespace
