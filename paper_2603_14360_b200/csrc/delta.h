@@ -50,6 +50,7 @@ struct DeltaArgs {
   const int32_t *cu;
   int nch;                     // chunks of the longest sequence
   int per_q, per_k;            // heads to a q head, to a k head
+  int sms;                     // chains: SMs of the device
   int hpc, wv;                 // chains: heads and 16-column warps per head of a CTA; gradient kernel: heads of a CTA
 };
 

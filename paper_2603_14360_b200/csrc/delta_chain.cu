@@ -264,11 +264,21 @@ __device__ __forceinline__ void rows_out(const float (&x)[4][4], uint32_t at, ui
 // Barriers of a CTA: stages filled and free
 struct ChainBars { uint64_t full[8], empty[8]; };
 
+// A warp's part: 0 .. nw - 1 a chain, nw copies, above that none.  An SM's CTAs come a layer after the other, and warp w of the SM's
+// belongs to scheduler w % 4: with CTAs of two warps (a chain) or four (two) the parts of every second pair of layers, or layer, change
+// places, so that chains share a scheduler only where there are more than four to the SM.
+__device__ __forceinline__ int chain_role(const DeltaArgs &a, int nw) {
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), layer = (int)(blockIdx.x / (unsigned)a.sms);
+  if (nw == 1) return warp ^ (layer >> 1 & 1);
+  if (nw == 2) return warp ^ (layer & 1) << 1;
+  return warp;
+}
+
 // What both kernels' chain warps begin with
 #define CHAIN_BEGIN(tensor, stride, back)                                                                                                     \
   extern __shared__ __align__(128) unsigned char smem[];                                                                                      \
   __shared__ ChainBars bars;                                                                                                                  \
-  const int nw = a.hpc * a.wv, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;     \
+  const int nw = a.hpc * a.wv, warp = chain_role(a, nw), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;                                 \
   if (threadIdx.x == 0) {                                                                                                                     \
     for (int i = 0; i < stages; ++i) { mbar_init(bars.full + i, 33); mbar_init(bars.empty + i, nw); }                                         \
     fence_mbar_init();                                                                                                                        \
@@ -278,6 +288,7 @@ struct ChainBars { uint64_t full[8], empty[8]; };
   const ChainWork w = chain_work(a, smem);                                                                                                    \
   const DeltaSpan sp = delta_span<C>(a, w.b);                                                                                                 \
   const uint32_t ring = smem_u32(smem), sb = (uint32_t)stage_bytes(K, nw, a.hpc);                                                             \
+  if (warp > nw) return;                                                                                                                      \
   if (warp == nw) {                                                                                                                           \
     chain_fill<K>(a, w, sp, tensor, stride, nw, stages, ring, bars.full, bars.empty, lane, back);                                             \
     return;                                                                                                                                   \
@@ -514,13 +525,17 @@ __global__ void __launch_bounds__(160, 2) delta_chain_bwd_kernel(DeltaArgs a, in
   if (a.dh0) state_out<K>(S, a.dh0, st_at, a.state_bf16, V, g, c);
 }
 
-// 16-column warps of a CTA.  A state's columns stay together (they share the copies of k, q and the records), up to four,
-// while there are CTAs for all SMs; with fewer units they are spread.
+// 16-column warps of a CTA: one, two or four, as leaves the fewest chains to a scheduler (see chain_role), and of those the most (they
+// share the copies of k, q and the records).
 ChainPlan plan_chain(const DeltaArgs &a) {
   const int cols = a.V / 16;
   const long long units = (long long)a.B * a.N, sms = sm_count();
-  ChainPlan p{1, cols < 4 ? cols : 4, 1, 4, 0};
-  while (p.wv > 1 && units * (cols / p.wv) < sms) p.wv /= 2;
+  ChainPlan p{1, 1, 1, 4, 0};
+  long long least = -1;
+  for (int wv = cols < 4 ? cols : 4; wv >= 1; wv /= 2) {
+    const long long layers = (units * (cols / wv) + sms - 1) / sms, load = wv == 4 ? layers : (layers * wv + 3) / 4;
+    if (least < 0 || load < least) { least = load; p.wv = wv; }
+  }
   p.slabs = cols / p.wv;
   const int nw = p.hpc * p.wv;
   // two CTAs to an SM where there are that many
@@ -533,11 +548,11 @@ ChainPlan plan_chain(const DeltaArgs &a) {
 template <int K> cudaError_t launch_k(const DeltaArgs &args, bool backward, cudaStream_t s) {
   DeltaArgs a = args;
   const ChainPlan p = plan_chain(a);
-  a.hpc = p.hpc; a.wv = p.wv;
+  a.hpc = p.hpc; a.wv = p.wv; a.sms = sm_count();
   void (*kernel)(DeltaArgs, int) = backward ? delta_chain_bwd_kernel<K> : !a.states ? delta_chain_fwd_kernel<K, true, false> : a.y ? delta_chain_fwd_kernel<K, true, true> : delta_chain_fwd_kernel<K, false, true>;
   const cudaError_t e = allow_smem(kernel, p.smem);
   if (e != cudaSuccess) return e;
-  return launch_early(kernel, dim3((unsigned)((long long)a.B * (a.N / p.hpc) * p.slabs)), dim3(32 * (p.hpc * p.wv + 1)), p.smem, s, a, p.stages);
+  return launch_early(kernel, dim3((unsigned)((long long)a.B * (a.N / p.hpc) * p.slabs)), dim3(p.wv == 2 ? 128 : 32 * (p.wv + 1)), p.smem, s, a, p.stages);
 }
 cudaError_t launch(const DeltaArgs &a, bool backward, cudaStream_t s) {
   switch (a.K) {

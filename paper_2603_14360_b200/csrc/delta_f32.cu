@@ -5,7 +5,7 @@
 //   chain: columns of the state are independent recurrences.  Sixteen lanes have a column, K/16 rows each in registers.  Their
 //          sixteen partial products with the chunk's tokens are added by recursive halving, which leaves token t's sum in
 //          lane t: the products with T and P and with the tokens are then FMAs on shuffled values.  A CTA's warps share the
-//          chunk's rows in shared memory (two stages, cp.async); few columns to a CTA where there are few units.
+//          chunk's rows in shared memory (stages that a warp of its own fills by cp.async); few columns to a CTA where there are few units.
 //   grad : a CTA a chunk of one head, everything of it in shared memory; four tokens' entries of a feature to a thread.
 // States of chunks are kept column after column, [V][K], so that a column's lanes write contiguous floats.
 #include "delta_common.cuh"
@@ -147,17 +147,16 @@ template <int M> __device__ __forceinline__ void rows_to(float *p, const float (
   }
 }
 // Sums of p[t] over the sixteen lanes of a column; lane t keeps p[t]'s
-__device__ __forceinline__ float halve(float (&p)[C], int l) {
+template <int H> __device__ __forceinline__ float halve(const float (&p)[2 * H], int l) {
+  const bool up = l & H;
+  float q[H];
 #pragma unroll
-  for (int h = 8; h; h /= 2) {
-    const bool up = l & h;
-#pragma unroll
-    for (int i = 0; i < h; ++i) {
-      const float send = up ? p[i] : p[h + i], keep = up ? p[h + i] : p[i];
-      p[i] = keep + __shfl_xor_sync(0xffffffffu, send, h);
-    }
+  for (int i = 0; i < H; ++i) {
+    const float send = up ? p[i] : p[H + i], keep = up ? p[H + i] : p[i];
+    q[i] = keep + __shfl_xor_sync(0xffffffffu, send, H);
   }
-  return p[0];
+  if constexpr (H > 1) return halve<H / 2>(q, l);
+  else return q[0];
 }
 // token t's product rows . S of this lane's column
 template <int M> __device__ __forceinline__ float dots(const float *rows, int pitch, const float (&S)[M], int l) {
@@ -170,68 +169,83 @@ template <int M> __device__ __forceinline__ float dots(const float *rows, int pi
 #pragma unroll
     for (int m = 0; m < M; ++m) p[t] = fmaf(x[m], S[m], p[t]);
   }
-  return halve(p, l);
+  return halve<C / 2>(p, l);
 }
 
-constexpr int kStages = 2, kPM = 20;      // pitch of T and P in shared memory: rows as float4 and columns without conflicts
+constexpr int kStages = 4, kPM = 20;      // pitch of T and P in shared memory: rows as float4 and columns without conflicts
 // Shared memory of a stage (floats): k, q rows, T, P, vectors, nc columns of v (dy)
 constexpr int kSP = C * kPM, kSVec = 2 * C * kPM, kSRec = kSVec + 8 * C;
 __host__ __device__ constexpr int f32_stage(int K, int nc) { return 2 * C * K + kSRec + C * nc; }
 
-// Chunk `ch` on its way into stage `st`; nc (columns of the CTA) a power of two, 16 threads to a column
+// The copying warp's loop; nc (columns of the CTA) 4, 8 or 16.  A lane has a place in a row for good.
 template <int K>
-__device__ __forceinline__ void f32_fill(const DeltaArgs &a, const DeltaSpan &sp, int n, int col0, int log_nc, int ch, float *st, const float *kg, const float *qg,
-                                         const float *vg, long long vs) {
-  const int tid = threadIdx.x, nt = 16 << log_nc;
-  const long long tok = (long long)ch * C;
-  const int have = min(C, sp.T - ch * C);
-  for (int x = tid; x < C * (K / 4); x += nt) {
-    const int r = x / (K / 4), o = 4 * (x % (K / 4));
-    const bool ok = r < have;
-    cp16_or_zero(smem_u32(st + r * K + o), kg + (tok + (ok ? r : 0)) * a.ks + o, ok);
-    cp16_or_zero(smem_u32(st + (C + r) * K + o), qg + (tok + (ok ? r : 0)) * a.qs + o, ok);
-  }
-  const float *rec = reinterpret_cast<const float *>(a.rec) + ((size_t)(sp.slot0 + ch) * a.N + n) * kRec;
-  float *sr = st + 2 * C * K;
-  for (int x = tid; x < 2 * C * C / 4; x += nt) cp16(smem_u32(sr + (x >> 2) * kPM + 4 * (x & 3)), rec + 4 * x);      // (T, then P)
-  for (int x = tid; x < 2 * C; x += nt) cp16(smem_u32(sr + kSVec + 4 * x), rec + kVec + 4 * x);
-  const int lp = log_nc - 2;
-  for (int x = tid; x < C << lp; x += nt) {
-    const int r = x >> lp, o = 4 * (x & ((1 << lp) - 1));
-    const bool ok = r < have;
-    cp16_or_zero(smem_u32(sr + kSRec + (r << log_nc) + o), vg + (tok + (ok ? r : 0)) * vs + o, ok);
+__device__ __forceinline__ void f32_fill(const DeltaArgs &a, const DeltaSpan &sp, int n, int col0, int nc, float *ring, const float *vg, long long vs, uint64_t *full,
+                                         uint64_t *empty, int lane, bool backward) {
+  constexpr int P = K / 4, LR = P % 32 == 0 ? 32 : P % 16 == 0 ? 16 : P % 8 == 0 ? 8 : 4, RP = 32 / LR;      // pieces, lanes to a row; rows to a pass
+  const int lv = nc / 4, rv = 32 / lv, r0 = lane / LR, rv0 = lane / lv;
+  const float *kp = static_cast<const float *>(a.k) + (sp.tok0 + r0) * a.ks + n / a.per_k * K + 4 * (lane % LR);
+  const float *qp = static_cast<const float *>(a.q) + (sp.tok0 + r0) * a.qs + n / a.per_q * K + 4 * (lane % LR);
+  const float *vp = vg + (sp.tok0 + rv0) * vs + (long long)n * a.V + col0 + 4 * (lane % lv);
+  const float *rp = reinterpret_cast<const float *>(a.rec) + ((size_t)sp.slot0 * a.N + n) * kRec + 4 * lane;
+  for (int i = 0; i < sp.n; ++i) {
+    const int ch = backward ? sp.n - 1 - i : i, st = i % kStages, have = min(C, sp.T - ch * C);
+    if (i >= kStages && !mbar_wait<64>(empty + st, (uint32_t)((i / kStages - 1) & 1))) {
+      if (lane == 0) report_timeout(a.dev_status);
+      for (int o = i - kStages; o < i; ++o) (void)mbar_wait(full + o % kStages, (uint32_t)((o / kStages) & 1));   // its copies on their way
+      return;
+    }
+    float *base = ring + st * f32_stage(K, nc), *sr = base + 2 * C * K;
+    const uint32_t kd = smem_u32(base + r0 * K + 4 * (lane % LR));
+    const float *ks = kp + (long long)ch * C * a.ks, *qs = qp + (long long)ch * C * a.qs, *vv = vp + (long long)ch * C * vs, *rs = rp + (size_t)ch * a.N * kRec;
+#pragma unroll
+    for (int p = 0; p < C / RP; ++p, ks += RP * a.ks, qs += RP * a.qs) {
+      const bool ok = r0 + p * RP < have;      // rows behind the last token are zeros
+#pragma unroll
+      for (int x = 0; x < P / LR; ++x) {
+        cp16_or_zero(kd + 4 * (p * RP * K + 4 * LR * x), ok ? ks + 4 * LR * x : static_cast<const float *>(a.k), ok);
+        cp16_or_zero(kd + 4 * ((C + p * RP) * K + 4 * LR * x), ok ? qs + 4 * LR * x : static_cast<const float *>(a.q), ok);
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x) cp16(smem_u32(sr + (8 * x + (lane >> 2)) * kPM + 4 * (lane & 3)), rs + 128 * x);      // (T, then P)
+    cp16(smem_u32(sr + kSVec + 4 * lane), rs + kVec);
+#pragma unroll 1
+    for (int r = rv0; r < C; r += rv, vv += rv * vs) cp16_or_zero(smem_u32(sr + kSRec + r * nc + 4 * (lane % lv)), r < have ? vv : vg, r < have);
+    cp_arrive(full + st);
   }
 }
-#define F32_COMMIT() asm volatile("cp.async.commit_group;" ::: "memory")
 
 template <int M, bool BWD>
-__global__ void __launch_bounds__(256) delta_chain_f32_kernel(DeltaArgs a) {
+__global__ void __launch_bounds__(288) delta_chain_f32_kernel(DeltaArgs a, int nc) {
   extern __shared__ __align__(16) float sm[];
+  __shared__ uint64_t full[kStages], empty[kStages];
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) { mbar_init(full + i, 32); mbar_init(empty + i, nc / 2); }
+    fence_mbar_init();
+  }
   begin_dependent();
+  __syncthreads();
   constexpr int K = 16 * M;
-  const int nc = blockDim.x / 16, V = a.V, slabs = V / nc, lane = threadIdx.x & 31, l = lane & 15, base = lane & 16;
+  const int V = a.V, slabs = V / nc, lane = threadIdx.x & 31, l = lane & 15, base = lane & 16;
   const int unit = blockIdx.x / slabs, b = unit / a.N, n = unit % a.N, col0 = blockIdx.x % slabs * nc, mine = threadIdx.x / 16, v = col0 + mine;
   const DeltaSpan sp = delta_span<C>(a, b);
+  if (mine >= nc) {      // (the last warp)
+    f32_fill<K>(a, sp, n, col0, nc, sm, static_cast<const float *>(BWD ? a.dy : a.v), BWD ? (long long)a.N * V : a.vs, full, empty, lane, BWD);
+    return;
+  }
   const size_t at = ((size_t)b * a.N + n) * K * V + v;
   const void *in = BWD ? a.d_hT : a.h0;
   void *out = BWD ? a.dh0 : a.hT;
   float S[M];      // rows M l ..
 #pragma unroll
   for (int m = 0; m < M; ++m) S[m] = in ? load_state(in, at + (size_t)(M * l + m) * V, a.state_bf16) : 0.f;
-  const long long vs = BWD ? (long long)a.N * V : a.vs;
-  const float *vg = static_cast<const float *>(BWD ? a.dy : a.v) + sp.tok0 * vs + (long long)n * V + col0;
-  const float *kg = static_cast<const float *>(a.k) + sp.tok0 * a.ks + (long long)(n / (a.N / a.Nk)) * K;
-  const float *qg = static_cast<const float *>(a.q) + sp.tok0 * a.qs + (long long)(n / (a.N / a.Nq)) * K;
-  const int stage = f32_stage(K, nc), log_nc = 31 - __clz(nc);
-  if (sp.n > 0) f32_fill<K>(a, sp, n, col0, log_nc, BWD ? sp.n - 1 : 0, sm, kg, qg, vg, vs);
-  F32_COMMIT();
   for (int i = 0; i < sp.n; ++i) {
-    const int ch = BWD ? sp.n - 1 - i : i, have = min(C, sp.T - ch * C);
-    if (i + 1 < sp.n) f32_fill<K>(a, sp, n, col0, log_nc, BWD ? ch - 1 : ch + 1, sm + ((i + 1) & 1) * stage, kg, qg, vg, vs);
-    F32_COMMIT();
-    asm volatile("cp.async.wait_group 1;" ::: "memory");
-    __syncthreads();
-    const float *ks = sm + (i & 1) * stage, *qs = ks + C * K, *rec = qs + C * K, *vec = rec + kSVec, *vt = rec + kSRec;
+    const int ch = BWD ? sp.n - 1 - i : i, st = i % kStages, have = min(C, sp.T - ch * C);
+    if (!mbar_wait(full + st, (uint32_t)((i / kStages) & 1))) {
+      if (lane == 0) report_timeout(a.dev_status);
+      return;
+    }
+    const float *ks = sm + st * f32_stage(K, nc), *qs = ks + C * K, *rec = qs + C * K, *vec = rec + kSVec, *vt = rec + kSRec;
     const long long tok = sp.tok0 + ch * C;
     const size_t slot = (size_t)(sp.slot0 + ch) * a.N + n;
     const float x0 = vt[l * nc + mine], ec = expf(vec[C * kVecG + C - 1]);
@@ -284,9 +298,9 @@ __global__ void __launch_bounds__(256) delta_chain_f32_kernel(DeltaArgs a) {
         for (int m = 0; m < M; ++m) S[m] = fmaf(q[m], ej, fmaf(k[m], fj, S[m]));
       }
     }
-    __syncthreads();      // (the stage is the next but one's)
+    __syncwarp();
+    if (lane == 0) mbar_arrive(empty + st);
   }
-  asm volatile("cp.async.wait_all;" ::: "memory");
   if (out)
 #pragma unroll
     for (int m = 0; m < M; ++m) store_state(out, at + (size_t)(M * l + m) * V, a.state_bf16, S[m]);
@@ -490,7 +504,7 @@ template <int M, bool BWD> cudaError_t chain_m(const DeltaArgs &a, cudaStream_t 
   const size_t smem = (size_t)kStages * f32_stage(a.K, nc) * sizeof(float);
   const cudaError_t e = allow_smem(delta_chain_f32_kernel<M, BWD>, smem);
   if (e != cudaSuccess) return e;
-  return launch_early(delta_chain_f32_kernel<M, BWD>, dim3((unsigned)(units * (a.V / nc))), dim3(16 * nc), smem, s, a);
+  return launch_early(delta_chain_f32_kernel<M, BWD>, dim3((unsigned)(units * (a.V / nc))), dim3(16 * nc + 32), smem, s, a, nc);
 }
 template <bool BWD> cudaError_t chain(const DeltaArgs &a, cudaStream_t s) {
   switch (a.K) {
