@@ -5,18 +5,21 @@
 // pool (a compaction shifts, a permutation swaps): a CTA takes a slab of P x 16 bytes of every row, the same bytes of
 // each, holds the n pieces of it in registers, and writes them after a barrier.  Slabs do not touch one another, so
 // nothing has to be ordered between CTAs and no byte passes through scratch.  P is as large as 64 KB of a CTA allow
-// (16 pieces of 16 bytes a thread), a row's slab at least 32 bytes, a sector: that bounds n.
+// (16 pieces of 16 bytes a thread, or 8), a row's slab at least 32 bytes, a sector: that bounds n.
 // Where a destination comes twice the last pair counts; each CTA finds those once (n^2 / 256 comparisons a thread) and
 // walks several slabs.
+// Few pairs (rows' pieces stay wide): eight pieces a thread and four CTAs to an SM, which load while others store (8 states of 344 KB in 24
+// layers from one: 14.9 us, with sixteen and two 19.1); many: sixteen and two (200 of 512 states of 1 MB: 63 us, 77 the other way).
 #include "delta.h"
 #include "internal.h"
 
 namespace m2rnn {
 namespace {
 
-constexpr int kThreads = 256, kPer = 16, kMost = kThreads * kPer / 2;
+constexpr int kThreads = 256, kMost = kThreads * 16 / 2, kFew = 64;      // pairs: most, and up to which eight pieces a thread do
 
-__global__ void __launch_bounds__(kThreads, 2) state_copy_kernel(StateCopyArgs a, int log_p, int slabs) {
+template <int kPer>
+__global__ void __launch_bounds__(kThreads, 32 / kPer) state_copy_kernel(StateCopyArgs a, int log_p, int slabs) {
   __shared__ int from[kMost], to[kMost];
   begin_dependent();
   const int tid = threadIdx.x, P = 1 << log_p;      // pieces of a slab
@@ -70,15 +73,16 @@ __global__ void __launch_bounds__(kThreads, 2) state_copy_kernel(StateCopyArgs a
 
 int state_copy_limit() { return kMost; }
 
-cudaError_t launch_state_copy(const StateCopyArgs &a, cudaStream_t s) {
+template <int kPer> static cudaError_t launch_per(const StateCopyArgs &a, cudaStream_t s) {
   // the widest slab whose n pieces a CTA holds; no wider than a row, nor (down to 512 bytes) than leaves a slab for each CTA
-  const long long most = (long long)sm_count() * 2;
+  const long long most = (long long)sm_count() * (32 / kPer);
   auto slabs_of = [&](int l) { return (a.row_bytes + (16ll << l) - 1) / (16ll << l) * a.layers; };
   int log_p = 1;
   while (((long long)a.n << (log_p + 1)) <= kThreads * kPer && (16ll << log_p) < a.row_bytes && (log_p < 5 || slabs_of(log_p + 1) >= most)) ++log_p;
   const long long slabs = slabs_of(log_p);
   if (slabs > 0x7fffffffll) return cudaErrorInvalidValue;
-  return launch_early(state_copy_kernel, dim3((unsigned)(slabs < most ? slabs : most)), dim3(kThreads), 0, s, a, log_p, (int)slabs);
+  return launch_early(state_copy_kernel<kPer>, dim3((unsigned)(slabs < most ? slabs : most)), dim3(kThreads), 0, s, a, log_p, (int)slabs);
 }
+cudaError_t launch_state_copy(const StateCopyArgs &a, cudaStream_t s) { return a.n <= kFew ? launch_per<8>(a, s) : launch_per<16>(a, s); }
 
 }  // namespace m2rnn
