@@ -12,7 +12,6 @@
 namespace m2rnn {
 namespace {
 
-constexpr int kWarps = 8;      // of a CTA
 
 // 16 bytes of a state, as they lie in memory, and as floats
 template <typename TS> struct Vec16;
@@ -33,9 +32,9 @@ template <> struct Vec16<__nv_bfloat16> {
   __device__ static uint4 close(const float (&x)[8]) { return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])); }
 };
 
-// R: 16-byte pieces of a lane, most; W warps to a unit
-template <typename TIO, typename TS, int V, int R>
-__global__ void __launch_bounds__(32 * kWarps, R > 8 ? 2 : 3) delta_step_kernel(DeltaStepArgs a, int W) {
+// R: 16-byte pieces of a lane, most; W warps to a unit, kWarps to a CTA
+template <typename TIO, typename TS, int V, int R, int kWarps>
+__global__ void __launch_bounds__(32 * kWarps, (R > 8 ? 16 : 28) / kWarps) delta_step_kernel(DeltaStepArgs a, int W) {
   using X = Vec16<TS>;
   constexpr int E = X::n, L = V / E, G = 32 / L;     // lanes to a row, rows of a warp at a time
   __shared__ float part[kWarps][2][V];               // sums over a warp's rows; then [unit's first warp][0]: u
@@ -154,15 +153,19 @@ __global__ void __launch_bounds__(32 * kWarps, R > 8 ? 2 : 3) delta_step_kernel(
 template <typename TIO, typename TS, int V> cudaError_t launch_v(const DeltaStepArgs &a, cudaStream_t s) {
   constexpr int E = Vec16<TS>::n, G = 32 / (V / E), R = sizeof(TS) == 4 ? 16 : 8;      // 64 entries of a state a lane, most
   // warps to a unit: a power of two that leaves whole groups of rows and at most R pieces a lane
+  constexpr int most = 8;
   int W = 1;
-  while (W < kWarps && a.K / (G * W) > R) W *= 2;
+  while (W < most && a.K / (G * W) > R) W *= 2;
   const long long units = (long long)a.B * a.N;
   // few units: more warps to each, while every one has a group of rows
-  while (W < kWarps && a.K % (2 * W * G) == 0 && units * W * 2 <= (long long)sm_count() * kWarps) W *= 2;
-  const long long grid = (units + kWarps / W - 1) / (kWarps / W);
-  const dim3 g((unsigned)grid), t(32 * kWarps);
-  if (a.K / (G * W) <= R / 2) return launch_early(delta_step_kernel<TIO, TS, V, R / 2>, g, t, 0, s, a, W);
-  return launch_early(delta_step_kernel<TIO, TS, V, R>, g, t, 0, s, a, W);
+  while (W < most && a.K % (2 * W * G) == 0 && units * W * 2 <= (long long)sm_count() * 8) W *= 2;
+  // CTAs of four warps fill an SM's registers closer than those of eight (28 warps against 24: the units of 48 sequences of 84 heads at
+  // once instead of in two rounds)
+  const int warps = W > 4 ? 8 : 4;
+  const dim3 g((unsigned)((units * W + warps - 1) / warps)), t(32 * warps);
+  const bool half = a.K / (G * W) <= R / 2;
+  if (warps == 8) return half ? launch_early(delta_step_kernel<TIO, TS, V, R / 2, 8>, g, t, 0, s, a, W) : launch_early(delta_step_kernel<TIO, TS, V, R, 8>, g, t, 0, s, a, W);
+  return half ? launch_early(delta_step_kernel<TIO, TS, V, R / 2, 4>, g, t, 0, s, a, W) : launch_early(delta_step_kernel<TIO, TS, V, R, 4>, g, t, 0, s, a, W);
 }
 template <typename TIO, typename TS> cudaError_t launch_t(const DeltaStepArgs &a, cudaStream_t s) {
   switch (a.V) {
