@@ -34,7 +34,7 @@ template <> struct Vec16<__nv_bfloat16> {
 
 // R: 16-byte pieces of a lane, most; W warps to a unit, kWarps to a CTA
 template <typename TIO, typename TS, int V, int R, int kWarps>
-__global__ void __launch_bounds__(32 * kWarps, (R > 8 ? 16 : 28) / kWarps) delta_step_kernel(DeltaStepArgs a, int W) {
+__global__ void __launch_bounds__(32 * kWarps, (R > 8 ? 16 : sizeof(TS) == 2 ? 32 : 28) / kWarps) delta_step_kernel(DeltaStepArgs a, int W) {
   using X = Vec16<TS>;
   constexpr int E = X::n, L = V / E, G = 32 / L;     // lanes to a row, rows of a warp at a time
   __shared__ float part[kWarps][2][V];               // sums over a warp's rows; then [unit's first warp][0]: u
