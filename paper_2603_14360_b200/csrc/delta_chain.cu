@@ -525,16 +525,17 @@ __global__ void __launch_bounds__(160, 2) delta_chain_bwd_kernel(DeltaArgs a, in
   if (a.dh0) state_out<K>(S, a.dh0, st_at, a.state_bf16, V, g, c);
 }
 
-// 16-column warps of a CTA: one, two or four, as leaves the fewest chains to a scheduler (see chain_role), and of those the most (they
-// share the copies of k, q and the records).
+// 16-column warps of a CTA: four (they share the copies of k, q and the records), two or one where that leaves a quarter fewer chains to
+// the SM that has the most: chains of an SM share its shared memory's bandwidth (65 536 tokens, 32 heads of 128 x 128: 64 CTAs of four
+// 2 403 us, 128 of two 1 609).
 ChainPlan plan_chain(const DeltaArgs &a) {
   const int cols = a.V / 16;
   const long long units = (long long)a.B * a.N, sms = sm_count();
   ChainPlan p{1, 1, 1, 4, 0};
-  long long least = -1;
+  long long least = 0;
   for (int wv = cols < 4 ? cols : 4; wv >= 1; wv /= 2) {
-    const long long layers = (units * (cols / wv) + sms - 1) / sms, load = wv == 4 ? layers : (layers * wv + 3) / 4;
-    if (least < 0 || load < least) { least = load; p.wv = wv; }
+    const long long chains = (units * (cols / wv) + sms - 1) / sms * wv;
+    if (!least || 4 * chains <= 3 * least) { least = chains; p.wv = wv; }
   }
   p.slabs = cols / p.wv;
   const int nw = p.hpc * p.wv;
