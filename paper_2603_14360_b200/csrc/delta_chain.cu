@@ -30,8 +30,9 @@ __host__ __device__ constexpr int pitch_k(int K) { return 2 * K + 16; }
 __host__ __device__ constexpr int pitch_v(int nw) { return 32 * nw + 16; }
 __host__ __device__ constexpr int stage_bytes(int K, int nw, int heads) { return C * (2 * pitch_k(K) + pitch_v(nw)) + heads * kRecChain; }
 
-// Forward, a chain warp's S as operands, blocks [column tile][feature tile]
-__host__ __device__ constexpr int out_bytes(int K) { return 32 * K; }
+// Forward, a chain warp's S as operands of the next chunk's pass (Y): in registers where K leaves them, else in shared memory, blocks
+// [column tile][feature tile].  (Shared memory's bandwidth is what chains of an SM compete for: 324 of its cycles a chain and chunk of K = 64.)
+__host__ __device__ constexpr int out_bytes(int K) { return K <= 64 ? 0 : 32 * K; }
 
 struct ChainPlan { int hpc, wv, slabs, stages; size_t smem; };
 
@@ -314,7 +315,7 @@ __global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, in
   __nv_bfloat16 *yg = Y ? static_cast<__nv_bfloat16 *>(a.y) + ((size_t)(sp.tok0 + lane) * a.N + n) * V + v0 : nullptr;
   char *sg = KEEP ? a.states + ((size_t)sp.slot0 * a.N + n) * (2 * K * V) + 2 * K * v0 + 4 * lane : nullptr, *ug = KEEP ? a.upd + ((size_t)sp.slot0 * a.N + n) * (2 * C * V) + 2 * C * v0 + 4 * lane : nullptr;
   const uint32_t s_at = out + 16 * l.row + 128 * (l.mat_lo * (K / 8) + l.mat_hi);      // tiles of S: 256 bytes apart
-  uint32_t Ub[2][4] = {};      // U as operands
+  uint32_t Ub[2][4] = {}, Sb[K <= 64 ? K / 16 : 1][4] = {};      // U, S as operands
   float y[4][4];
   // Y from q S: scaled, + P U
   auto y_rest = [&](uint32_t stage) {
@@ -345,12 +346,12 @@ __global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, in
     zero(acc);
     zero(y);
     uint32_t fo[2][4];      // the chunk before's S
-    if (Y) ldmatrix_x4(s_at, fo[0]);
+    if (Y && K > 64) ldmatrix_x4(s_at, fo[0]);
 #pragma unroll
     for (int kt = 0; kt < K / 16; ++kt) {
       uint32_t f[4];
       pack_a<K / 8>(S, kt, f);
-      if (Y) {
+      if (Y && K > 64) {
         if (kt + 1 < K / 16) ldmatrix_x4(s_at + 256 * (kt + 1), fo[(kt + 1) & 1]);
         stmatrix_x4(s_at + 256 * kt, f);
       }
@@ -358,7 +359,15 @@ __global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, in
 #pragma unroll
       for (int r = 0; r < 4; ++r) { S[2 * kt][r] *= ec; S[2 * kt + 1][r] *= ec; }
       kb.step(acc, f, kt);
-      if (Y) qb.step(y, fo[kt & 1], kt);
+      if (Y) {
+        if constexpr (K > 64) {
+          qb.step(y, fo[kt & 1], kt);
+        } else {
+          qb.step(y, Sb[kt], kt);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) Sb[kt][r] = f[r];
+        }
+      }
     }
     if (Y) y_rest(last);
     // X
@@ -416,9 +425,13 @@ __global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, in
     zero(y);
 #pragma unroll
     for (int kt = 0; kt < K / 16; ++kt) {
-      uint32_t f[4];
-      ldmatrix_x4(s_at + 256 * kt, f);
-      qb.step(y, f, kt);
+      if constexpr (K > 64) {
+        uint32_t f[4];
+        ldmatrix_x4(s_at + 256 * kt, f);
+        qb.step(y, f, kt);
+      } else {
+        qb.step(y, Sb[kt], kt);
+      }
     }
     y_rest(last);
     rows_out(y, last + v_at, last + v_mine, pv, yg, lane < sp.T - (sp.n - 1) * C);
