@@ -37,7 +37,7 @@ template <int K, int KG> struct GradCfg {
   static constexpr int NT = (K / 8 + KG - 1) / KG;                       // 8-feature tiles of a warp, most
   static constexpr int JT = 4 / KG;                                      // 8-token tiles of a warp's part of a 16 x 32 product
   // rows of 32 floats: a1, a2, a3 by part of the features; sums of X1 (.) QK^T and X2 (.) KK^T / b over a row's entries by part of
-  // the tokens; over a column's by half; X1 (.) QK^T's diagonal; L . v; the factors of the division by the lengths; <S, dS'> by warp
+  // the tokens; over a column's by half; X1 (.) QK^T's diagonal; L . v; the factors of the division by the lengths; <S, dS'>
   static constexpr int kA = 0, kRow1 = 3 * KG, kRow2 = 4 * KG, kCol = 5 * KG, kDiag = kCol + 2, kLv = kCol + 3, kUq = kCol + 4, kUk = kCol + 5, kSds = kCol + 6;
   static_assert(kSlab % 16 == 0, "");
 };
@@ -49,7 +49,7 @@ struct GradJob { long long tok; size_t slot; int have, n0, run, hq, hk; };      
 template <int K, int KG, bool MULTI, int VS, int BUFS, int CTAS>
 __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, unsigned jobs) {
   using Cfg = GradCfg<K, KG>;
-  constexpr int NT = Cfg::NT, JT = Cfg::JT, kThreads = Cfg::kThreads;
+  constexpr int NT = Cfg::NT, JT = Cfg::JT, kThreads = Cfg::kThreads, kIdle = 2 * (KG - 1);
   constexpr int pv = 2 * VS + 16, P = VS / 8, slab = slab_bytes(K, VS), UB = 2 * C * VS, SB = 2 * K * VS;      // P: pieces of a row; bytes of U, of S
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ uint64_t full[2];
@@ -88,12 +88,15 @@ __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, 
     }
     return o;
   };
-  // rows of q and k of a job, and slab `part` of its head n, on their way
+  // rows of q and k of a job, and slab `part` of its head n, on their way.
+  constexpr int NR = (C * (K / 8) + kThreads - 1) / kThreads, NV = (C * P + kThreads - 1) / kThreads;
   auto fetch_rows = [&](const GradJob &o, int qb) {
     const __nv_bfloat16 *kg = static_cast<const __nv_bfloat16 *>(a.k) + o.tok * a.ks + o.hk * K;
     const __nv_bfloat16 *qg = static_cast<const __nv_bfloat16 *>(a.q) + o.tok * a.qs + o.hq * K;
-    for (int x = tid; x < C * (K / 8); x += kThreads) {
-      const int r = x / (K / 8), p = x % (K / 8);
+#pragma unroll
+    for (int y = 0; y < NR; ++y) {
+      const int x = tid + y * kThreads, r = x / (K / 8), p = x % (K / 8);
+      if (C * (K / 8) % kThreads && x >= C * (K / 8)) break;
       const bool ok = r < o.have;
       const uint32_t at = base + qb * Cfg::kRows + r * Cfg::kPK + 16 * p;
       cp16_or_zero(at, qg + (ok ? r * a.qs : 0) + 8 * p, ok);
@@ -113,13 +116,12 @@ __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, 
       bulk_load(usa + 2 * UB + SB, a.dstates + x, SB, full + buf);
     }
     const __nv_bfloat16 *yg = static_cast<const __nv_bfloat16 *>(a.dy) + (o.tok * a.N + n) * V + vb, *vg = static_cast<const __nv_bfloat16 *>(a.v) + o.tok * a.vs + (long long)n * V + vb;
-    const long long ys = (long long)a.N * V;
 #pragma unroll
-    for (int x0 = 0; x0 < C * P; x0 += kThreads) {
-      const int x = x0 + tid, r = x / P, p = x % P;
+    for (int y = 0; y < NV; ++y) {
+      const int x = tid + y * kThreads, r = x / P, p = x % P;
       if (C * P % kThreads && x >= C * P) break;
       const bool ok = r < o.have;
-      cp16_or_zero(ysa + r * pv + 16 * p, yg + (ok ? r * ys : 0) + 8 * p, ok);
+      cp16_or_zero(ysa + r * pv + 16 * p, yg + (ok ? (long long)r * a.N * V : 0) + 8 * p, ok);
       cp16_or_zero(vsa + r * pv + 16 * p, vg + (ok ? r * a.vs : 0) + 8 * p, ok);
     }
   };
@@ -147,7 +149,7 @@ __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, 
 #pragma unroll
         for (int t = 0; t < NT; ++t) dq[t][r] = dm[t][r] = dp[t][r] = 0.f;
       }
-      float ss = 0.f;      // this thread's part of <S, dS'>
+      float ss = 0.f, ss1 = 0.f;      // this thread's part of <S, dS'>
       const float *vec = nullptr;
       for (int part = 0; part < parts; ++part, ++cnt) {
         const int bi = BUFS > 1 ? cnt & 1 : 0;
@@ -191,19 +193,6 @@ __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, 
               }
           }
         }
-        {      // <S, dS'>
-          const unsigned char *sp = buf + (ssa - at0);
-#pragma unroll
-          for (int x0 = 0; x0 < K * P; x0 += kThreads) {
-            const int x = x0 + tid;
-            if (K * P % kThreads && x >= K * P) break;
-            const uint4 p = *reinterpret_cast<const uint4 *>(sp + 16 * x), d = *reinterpret_cast<const uint4 *>(sp + SB + 16 * x);
-            ss = fma_bf16<0, 0>(p.x, d.x, fma_bf16<1, 1>(p.x, d.x, ss));
-            ss = fma_bf16<0, 0>(p.y, d.y, fma_bf16<1, 1>(p.y, d.y, ss));
-            ss = fma_bf16<0, 0>(p.z, d.z, fma_bf16<1, 1>(p.z, d.z, ss));
-            ss = fma_bf16<0, 0>(p.w, d.w, fma_bf16<1, 1>(p.w, d.w, ss));
-          }
-        }
         // products over the slab's columns
         const uint32_t y_at = ysa + (i0 + mrow + 8 * mlo) * pv + 16 * mhi, v_at = vsa + (8 * JT * kq + mrow) * pv + 16 * mlo;
         const uint32_t b_at = usa + 16 * mrow + 128 * (4 * mhi + 2 * mh + mlo), u_at = usa + 16 * mrow + 128 * (4 * mlo + JT * kq);   // blocks [column tile][token tile]
@@ -244,6 +233,17 @@ __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, 
             }
           }
         }
+        if (warp == kIdle) {      // <S, dS'>: the warp without a part of X1, X2 has the time
+          const unsigned char *sp = buf + (ssa - at0);
+#pragma unroll 4
+          for (int x = lane; x < K * P; x += 32) {
+            const uint4 p = *reinterpret_cast<const uint4 *>(sp + 16 * x), d = *reinterpret_cast<const uint4 *>(sp + SB + 16 * x);
+            ss = fma_bf16<0, 0>(p.x, d.x, fma_bf16<1, 1>(p.x, d.x, ss));
+            ss1 = fma_bf16<0, 0>(p.y, d.y, fma_bf16<1, 1>(p.y, d.y, ss1));
+            ss = fma_bf16<0, 0>(p.z, d.z, fma_bf16<1, 1>(p.z, d.z, ss));
+            ss1 = fma_bf16<0, 0>(p.w, d.w, fma_bf16<1, 1>(p.w, d.w, ss1));
+          }
+        }
         if (BUFS == 1 && part + 1 < parts) {
           __syncthreads();      // (the slab's place is the next one's)
           fetch(o, n, part + 1, 0);
@@ -269,8 +269,10 @@ __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, 
           const float t0 = x10 * qk[u][2 * x], t1 = x11 * qk[u][2 * x + 1], u0 = m0 * kk[u][2 * x], u1 = m1 * kk[u][2 * x + 1];
           c0 += fmaf(bt[x], u0, i > jj ? t0 : 0.f);
           c1 += fmaf(bt[x], u1, i > jj + 1 ? t1 : 0.f);
-          if (i == jj) { red[32 * Cfg::kDiag + i] = t0; red[32 * Cfg::kLv + i] = ld[u][2 * x]; }
-          if (i == jj + 1) { red[32 * Cfg::kDiag + i] = t1; red[32 * Cfg::kLv + i] = ld[u][2 * x + 1]; }
+          if (jt == 2 * mh + x && c == g >> 1) {      // the diagonal's entry of row i
+            red[32 * Cfg::kDiag + i] = g & 1 ? t1 : t0;
+            red[32 * Cfg::kLv + i] = g & 1 ? ld[u][2 * x + 1] : ld[u][2 * x];
+          }
           r1[x] += t0 + t1;
           r2[x] += u0 + u1;
           x1s[u][2 * x] = x10 + (MULTI && h ? x1s[u][2 * x] : 0.f);
@@ -319,9 +321,12 @@ __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, 
         red[32 * (Cfg::kA + KG * c + kq) + i] = c == 0 ? a1[x] : c == 1 ? a2[x] : c == 2 ? a3[x] : r1[x];      // (kRow1 follows a3)
         if (c == 0) red[32 * (Cfg::kRow2 + kq) + i] = r2[x];
       }
+      if (warp == kIdle) {
+        ss += ss1;
 #pragma unroll
-      for (int d = 16; d; d /= 2) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-      if (lane == 0) red[32 * Cfg::kSds + warp] = ss;
+        for (int d = 16; d; d /= 2) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+        if (lane == 0) red[32 * Cfg::kSds] = ss;
+      }
       if (!MULTI || h + 1 == a.hpc) {
 #pragma unroll
         for (int u = 0; u < JT; ++u) {
@@ -363,10 +368,7 @@ __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, 
         }
         if (lane < o.have) {
           const size_t at = (size_t)(o.tok + lane) * a.N + n;
-          float sd = 0.f;
-#pragma unroll
-          for (int x = 0; x < 2 * KG; ++x) sd += red[32 * Cfg::kSds + x];
-          const float dlog = fmaf(expf(vec[32 * kVecG + 31]), sd, part + all);
+          const float dlog = fmaf(expf(vec[32 * kVecG + 31]), red[32 * Cfg::kSds], part + all);
           static_cast<__nv_bfloat16 *>(a.dgate)[at] = __float2bfloat16_rn(dlog * vec[32 * kVecDlog + lane]);
           static_cast<__nv_bfloat16 *>(a.dstep)[at] = __float2bfloat16_rn((red[32 * Cfg::kLv + lane] - s2 + r2) * (a.step_kind == M2RNN_STEP_LOGIT ? b * (1.f - b) : 1.f));
         }
@@ -410,30 +412,27 @@ __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, 
     }
     __syncthreads();      // the factors are there; X1, X2, q and k are read
     if (BUFS == 1 && next.have) fetch(next, next.n0, 0, 0);
-    // through the division by the lengths: to the shares, or to the places of q and k
-    auto emit = [&](const float (&x)[NT][4], uint32_t at, int factors, float *part) {
-      if (part) part += ((size_t)(o.tok + i0 + g) * a.shares + o.run) * K + f0 + 2 * c;
+    // through the division by the lengths: to the shares, or to memory as they are (16 bytes of a row an instruction, two make a sector)
+    auto emit = [&](const float (&x)[NT][4], uint32_t at, int factors, float *part, void *out, int heads, int head) {
+      const size_t t = (size_t)(o.tok + i0 + g), step = (size_t)8 * (part ? a.shares : heads) * K;
+      float *pp = part + (t * a.shares + o.run) * K + f0 + 2 * c;
+      __nv_bfloat16 *po = static_cast<__nv_bfloat16 *>(out) + (t * heads + head) * K + f0 + 2 * c;
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
         const float f = red[32 * factors + i0 + g + 8 * y];
+        if (i0 + g + 8 * y >= o.have) continue;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          if (t >= tiles) continue;
-          const float2 was = unpack_bf16(__float_as_uint(lds32(at + 8 * y * Cfg::kPK + 16 * t)));
-          const float v0 = fmaf(f, was.x, x[t][2 * y]), v1 = fmaf(f, was.y, x[t][2 * y + 1]);
-          if (!part) sts32(at + 8 * y * Cfg::kPK + 16 * t, __uint_as_float(pack_bf16(v0, v1)));
-          else if (i0 + g + 8 * y < o.have) *reinterpret_cast<float2 *>(part + (size_t)8 * y * a.shares * K + 8 * t) = make_float2(v0, v1);
+        for (int u = 0; u < NT; ++u) {
+          if (u >= tiles) continue;
+          const float2 was = unpack_bf16(__float_as_uint(lds32(at + 8 * y * Cfg::kPK + 16 * u)));
+          const float v0 = fmaf(f, was.x, x[u][2 * y]), v1 = fmaf(f, was.y, x[u][2 * y + 1]);
+          if (part) *reinterpret_cast<float2 *>(pp + y * step + 8 * u) = make_float2(v0, v1);
+          else *reinterpret_cast<uint32_t *>(po + y * step + 8 * u) = pack_bf16(v0, v1);
         }
       }
     };
-    emit(dqs, qat, Cfg::kUq, a.dq_part);
-    emit(dks, kat, Cfg::kUk, a.dk_part);
-    __syncthreads();
-    for (int x = tid; x < o.have * (K / 8); x += kThreads) {
-      const int r = x / (K / 8), p = x % (K / 8);
-      if (!a.dq_part) *reinterpret_cast<float4 *>(static_cast<__nv_bfloat16 *>(a.dq) + ((size_t)(o.tok + r) * a.Nq + o.hq) * K + 8 * p) = lds128(qsa + r * Cfg::kPK + 16 * p);
-      if (!a.dk_part) *reinterpret_cast<float4 *>(static_cast<__nv_bfloat16 *>(a.dk) + ((size_t)(o.tok + r) * a.Nk + o.hk) * K + 8 * p) = lds128(ksa + r * Cfg::kPK + 16 * p);
-    }
+    emit(dqs, qat, Cfg::kUq, a.dq_part, a.dq, a.Nq, o.hq);
+    emit(dks, kat, Cfg::kUk, a.dk_part, a.dk, a.Nk, o.hk);
     if (!next.have) break;
     o = next;
   }
