@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(128) delta_prep_f32_kernel(DeltaArgs a) {
     for (int f = lane; f < K; f += 32) s = fmaf(row[f], row[f], s);
 #pragma unroll
     for (int d = 16; d; d /= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
-    if (lane == 0) vec[C * (r < C ? kVecRk : kVecRq) + r % C] = a.qk_norm ? 1.f / sqrtf(s + a.eps) : 1.f;
+    if (lane == 0) vec[C * (r < C ? kVecRk : kVecRq) + r % C] = !a.qk_norm ? 1.f : r % C < have ? 1.f / sqrtf(s + a.eps) : 0.f;      // (rows behind the last token: eps may be 0)
   }
   __syncthreads();
   float *rec = reinterpret_cast<float *>(a.rec) + ((size_t)(sp.slot0 + ch) * a.N + n) * kRec;

@@ -12,7 +12,8 @@
 // and as column of B.  T is inverted in fp32:
 // the two 16 x 16 blocks on the diagonal by forward substitution, a column a lane (a series of powers of M would
 // cancel digits where keys point the same way), then T_21 = -(T_22 M_21) T_11 with tf32 operands (2^-12 of each, before T is rounded to bf16).
-// (With q and k through shared memory, ldmatrix and the last product in FMA: 361 us against 205 for 65 536 tokens of 32 heads, K = 128.)
+// (65 536 tokens of 32 heads, K = 128, 1.4 GB: 251 us, 5.6 TB/s; with q and k through shared memory, the lengths by FMA and T's last
+// block too 361.)
 #include "delta_common.cuh"
 
 namespace m2rnn {
@@ -114,8 +115,9 @@ __global__ void __launch_bounds__(32 * kWarps, 4) delta_prep_kernel(DeltaArgs a,
       const int tile = x < 2 ? x : 2 + x, r = 2 * (x & 1);
       const float sk = __shfl_sync(0xffffffffu, g & 1 ? kk[tile][r + 1] : kk[tile][r], 4 * g + (g >> 1));
       const float sq = __shfl_sync(0xffffffffu, g & 1 ? qq[x][r + 1] : qq[x][r], 4 * g + (g >> 1));
-      rki[x] = rsqrtf(sk + a.eps);
-      rqi[x] = rsqrtf(sq + a.eps);
+      const bool row = 8 * x + g < have;      // (rows behind the last token: eps may be 0)
+      rki[x] = row ? rsqrtf(sk + a.eps) : 0.f;
+      rqi[x] = row ? rsqrtf(sq + a.eps) : 0.f;
     }
     rkj[x][0] = __shfl_sync(0xffffffffu, rki[x], 8 * c);
     rkj[x][1] = __shfl_sync(0xffffffffu, rki[x], 8 * c + 4);

@@ -558,10 +558,22 @@ PyObject *py_conv_silu_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
 
 // ---- gated delta rule and state copy
 
-// The call runs on its tensors' device, whichever is current, and on that device's stream.
-void *stream_on(PyObject *o, const at::Device &dev) {
-  return o == Py_None ? static_cast<void *>(c10::cuda::getCurrentCUDAStream(dev.index()).stream()) : stream_of(o);
-}
+// A call runs on its tensors' device, whichever is current, and on that device's current stream or the caller's; what it allocates
+// (outputs, workspace) belongs to that stream, so that the workspace is not handed out again before the kernels are done with it.
+struct On {
+  c10::cuda::OptionalCUDAStreamGuard other;
+  c10::cuda::OptionalCUDAGuard device;
+  void *stream;
+  On(PyObject *o, const at::Device &dev) {
+    if (o == Py_None) {
+      device.set_device(dev);
+      stream = c10::cuda::getCurrentCUDAStream(dev.index()).stream();
+    } else {
+      stream = stream_of(o);
+      other.reset_stream(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), dev.index()));
+    }
+  }
+};
 void same_device(const at::Device &dev, std::initializer_list<const Tensor *> ts) {
   for (const Tensor *t : ts)
     if (t && t->defined() && t->device() != dev) fail(PyExc_ValueError, "all tensors must be on one device: %s and %s", dev.str().c_str(), t->device().str().c_str());
@@ -629,7 +641,7 @@ PyObject *py_delta_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
   const Delta d = delta_call(q, k, v, gate, step, a + 6, cu, a[22], {h0, hT_given}, truth(a[15]) ? M2RNN_BF16 : M2RNN_F32);
   const m2rnn_delta_params &p = d.p;
   const at::Device dev = q.device();
-  const c10::cuda::CUDAGuard guard(dev);
+  const On on(a[20], dev);
   const ScalarType st = state_type(p.state_dtype);
   check(h0, "h0", {p.B, p.N, p.K, p.V}, st);
   const Tensor y = given_or_empty(opt_tensor(a[16], "y"), d.s.tok(p.N, p.V), d.s.io, dev);
@@ -648,12 +660,11 @@ PyObject *py_delta_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (const Tensor *t = opt_tensor(a[19], "workspace")) ws = *t;
   else if (const size_t need = m2rnn_delta_fwd_workspace_bytes(&p, ckpt.defined())) ws = empty({(int64_t)need}, ScalarType::Byte, dev);
   same_device(dev, {h0, &y, &hT, &ckpt, &ws});
-  void *stream = stream_on(a[20], dev);
   int32_t *status = status_of(q);
   int rc;
   Py_BEGIN_ALLOW_THREADS
   rc = m2rnn_delta_fwd(&p, ptr(q), ptr(k), ptr(v), ptr(gate), ptr(step), ptr(h0), fptr(d.o.alpha), fptr(d.o.beta), ptr(y), ptr(hT), ptr(ckpt), ptr(ws),
-                       ws.defined() ? ws.nbytes() : 0, status, stream);
+                       ws.defined() ? ws.nbytes() : 0, status, on.stream);
   Py_END_ALLOW_THREADS
   check_rc(rc, "m2rnn_delta_fwd");
   PyObject *r = PyTuple_New(3);
@@ -676,7 +687,7 @@ PyObject *py_delta_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
   const Delta d = delta_call(q, k, v, gate, step, a + 6, cu, a[27], {h0, d_hT, dh0_given}, truth(a[17]) ? M2RNN_BF16 : M2RNN_F32);
   const m2rnn_delta_params &p = d.p;
   const at::Device dev = q.device();
-  const c10::cuda::CUDAGuard guard(dev);
+  const On on(a[25], dev);
   const ScalarType st = state_type(p.state_dtype), io = d.s.io;
   check(h0, "h0", {p.B, p.N, p.K, p.V}, st);
   check(d_hT, "d_hT", {p.B, p.N, p.K, p.V}, st);
@@ -702,12 +713,11 @@ PyObject *py_delta_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (const Tensor *t = opt_tensor(a[18], "workspace")) ws = *t;
   else if (const size_t need = m2rnn_delta_bwd_workspace_bytes(&p, ckpt != nullptr)) ws = empty({(int64_t)need}, ScalarType::Byte, dev);
   same_device(dev, {h0, &dy, d_hT, ckpt, &dq, &dk, &dv, &dgate, &dstep, &dh0, &ws});
-  void *stream = stream_on(a[25], dev);
   int32_t *status = status_of(q);
   int rc;
   Py_BEGIN_ALLOW_THREADS
   rc = m2rnn_delta_bwd(&p, ptr(q), ptr(k), ptr(v), ptr(gate), ptr(step), ptr(h0), fptr(d.o.alpha), fptr(d.o.beta), ptr(ckpt), ptr(dy), ptr(d_hT), ptr(dq),
-                       ptr(dk), ptr(dv), ptr(dgate), ptr(dstep), ptr(dh0), ptr(ws), ws.defined() ? ws.nbytes() : 0, status, stream);
+                       ptr(dk), ptr(dv), ptr(dgate), ptr(dstep), ptr(dh0), ptr(ws), ws.defined() ? ws.nbytes() : 0, status, on.stream);
   Py_END_ALLOW_THREADS
   check_rc(rc, "m2rnn_delta_bwd");
   return dict_of({{"dq", a[19], &dq}, {"dk", a[20], &dk}, {"dv", a[21], &dv}, {"dgate", a[22], &dgate}, {"dstep", a[23], &dstep}, {"dh0", a[24], &dh0}});
@@ -739,16 +749,15 @@ PyObject *py_delta_decode_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
   check(o.alpha, "alpha", {p.N}, ScalarType::Float);
   check(o.beta, "beta", {p.N}, ScalarType::Float);
   const at::Device dev = q.device();
-  const c10::cuda::CUDAGuard guard(dev);
+  const On on(a[15], dev);
   const Tensor y = given_or_empty(opt_tensor(a[14], "y"), {p.B, p.N, p.V}, io, dev);
   check(y, "y", {p.B, p.N, p.V}, io);
   same_device(dev, {&k, &v, &gate, &step, &state, slots, o.alpha, o.beta, &y});
-  void *stream = stream_on(a[15], dev);
   int32_t *status = status_of(q);
   int rc;
   Py_BEGIN_ALLOW_THREADS
   rc = m2rnn_delta_decode_step(&p, ptr(q), ptr(k), ptr(v), ptr(gate), ptr(step), fptr(o.alpha), fptr(o.beta), ptr(state),
-                               static_cast<const int32_t *>(ptr(slots)), (int32_t)rows, ptr(y), status, stream);
+                               static_cast<const int32_t *>(ptr(slots)), (int32_t)rows, ptr(y), status, on.stream);
   Py_END_ALLOW_THREADS
   check_rc(rc, "m2rnn_delta_decode_step");
   return back(a[14], y);
@@ -782,13 +791,12 @@ PyObject *py_state_copy(PyObject *, PyObject *const *a, Py_ssize_t n) {
   same_device(dev, {&src, &to, &from});
   const char *d0 = static_cast<const char *>(ptr(dst)), *s0 = static_cast<const char *>(ptr(src));
   if ((d0 != s0 || src.size(axis) != dst.size(axis)) && d0 < s0 + src.nbytes() && s0 < d0 + dst.nbytes()) fail(PyExc_ValueError, "src and dst overlap without being the same");
-  const c10::cuda::CUDAGuard guard(dev);
-  void *stream = stream_on(a[5], dev);
+  const On on(a[5], dev);
   int32_t *status = status_of(dst);
   int rc;
   Py_BEGIN_ALLOW_THREADS
   rc = m2rnn_state_copy(ptr(dst), static_cast<const int32_t *>(ptr(to)), (int32_t)dst.size(axis), dst.size(axis) * row, ptr(src),
-                        static_cast<const int32_t *>(ptr(from)), (int32_t)src.size(axis), src.size(axis) * row, (int32_t)pairs, row, (int32_t)layers, status, stream);
+                        static_cast<const int32_t *>(ptr(from)), (int32_t)src.size(axis), src.size(axis) * row, (int32_t)pairs, row, (int32_t)layers, status, on.stream);
   Py_END_ALLOW_THREADS
   check_rc(rc, "m2rnn_state_copy");
   Py_INCREF(a[0]);

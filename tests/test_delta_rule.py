@@ -210,6 +210,37 @@ def test_chunks_of_a_prompt_and_repeats(dtype):
     assert all(torch.equal(a[n], b[n]) for n in a)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+def test_lengths_without_epsilon(dtype):
+    """norm_eps = 0: rows behind the last token, which are zeros, have no length to be divided by."""
+    x, on, H0, dy, d_hT, o = make(13, B=2, T=43, N=2, K=48, V=32, dtype=dtype)
+    o["norm_eps"] = 0.0
+    y_r, hT_r, g_r = ref.gradients([t.double() for t in x], H0.double(), dy.double(), d_hT.double(), **o)
+    y, hT, ckpt = m.m2rnn_delta_fwd(*on, H0.cuda(), save_ckpt=True, **on_gpu(o))
+    g = m.m2rnn_delta_bwd(*on, H0.cuda(), dy.cuda(), d_hT.cuda(), ckpt=ckpt, **on_gpu(o))
+    errs = dict(y=rel(y, y_r), hT=rel(hT, hT_r), **{n: rel(g[n], g_r[n]) for n in g_r})
+    assert max(errs.values()) <= TOL[dtype], errs
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+def test_rows_that_are_not_finite_stay_with_their_sequence(dtype):
+    """A NaN in one sequence, or behind a packed batch's tokens, reaches no other."""
+    x, on, H0, dy, d_hT, o = make(14, B=3, T=70, N=2, K=32, V=32, dtype=dtype)
+    o = on_gpu(o)
+    want = m.m2rnn_delta_fwd(*on, H0.cuda(), **o)[0]
+    for t in on:
+        t[1] = math.nan
+    y, hT, ckpt = m.m2rnn_delta_fwd(*on, H0.cuda(), save_ckpt=True, **o)
+    g = m.m2rnn_delta_bwd(*on, H0.cuda(), dy.cuda(), ckpt=ckpt, **o)
+    keep = [0, 2]
+    assert torch.equal(y[keep], want[keep]) and torch.isfinite(hT[keep]).all() and torch.isnan(y[1]).all()
+    assert all(torch.isfinite(v[keep]).all() for v in g.values())
+    flat = [t.flatten(0, 1)[:80].clone() for t in on]      # packed: sequences of 40 and 30 tokens, NaN in all that follows
+    cu = torch.tensor([0, 40, 70], dtype=torch.int32, device="cuda")
+    y, hT, _ = m.m2rnn_delta_fwd(*flat, cu_seqlens=cu, max_seqlen=40, **o)
+    assert torch.isfinite(y[:70]).all() and torch.isfinite(hT).all()
+
+
 def test_empty_calls():
     q = torch.zeros(2, 0, 2, 16, dtype=BF, device="cuda")
     v, gt = torch.zeros(2, 0, 2, 16, dtype=BF, device="cuda"), torch.zeros(2, 0, 2, dtype=BF, device="cuda")
