@@ -49,6 +49,7 @@ struct DeltaArgs {
   long long qs, ks, vs, TT;
   const int32_t *cu;
   int nch;                     // chunks of the longest sequence
+  long long slots;             // chunk slots of the batch
   int per_q, per_k;            // heads to a q head, to a k head
   int sms;                     // chains: SMs of the device
   int hpc, wv;                 // chains: heads and 16-column warps per head of a CTA; gradient kernel: heads of a CTA
@@ -73,6 +74,18 @@ template <int C> __device__ __forceinline__ DeltaSpan delta_span(const DeltaArgs
   }
   s.n = (s.T + C - 1) / C;
   return s;
+}
+// The batch entry that chunk slot `slot` belongs to (every lane of a warp calls it): of a packed batch the last one whose slots do not start
+// behind it.  (Jobs are numbered by slots: by entry and chunk of the longest, a ragged batch's were mostly none.)
+template <int C, bool PACKED> __device__ __forceinline__ int delta_entry(const DeltaArgs &a, unsigned slot) {
+  if (!PACKED) return (int)(slot / (unsigned)a.nch);
+  int b = -1;
+  for (int x = 0; x < a.B; x += 32) {
+    const int i = x + (int)(threadIdx.x & 31);
+    const bool in = i < a.B && min(max((long long)a.cu[i], 0ll), a.TT) / C + i <= slot;
+    b += __popc(__ballot_sync(0xffffffffu, in));
+  }
+  return __shfl_sync(0xffffffffu, b, 0);      // (known to be the same in all lanes: what derives from it stays in uniform registers)
 }
 #endif
 inline size_t delta_slots(const m2rnn_delta_params *p, size_t tokens, int C) {

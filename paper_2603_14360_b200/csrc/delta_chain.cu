@@ -18,6 +18,8 @@
 // chains have, so half the chains to an SM.)  What is kept for the gradient goes from registers to memory, 128 bytes an instruction.
 // Roundings to bf16: the operands S, X, U (dS, dU, L), the factored e^(g_last - g) U and the like, and T and P.  S itself
 // is held and updated in fp32.
+#include <algorithm>
+
 #include "delta_common.cuh"
 
 namespace m2rnn {
@@ -38,10 +40,13 @@ struct ChainPlan { int hpc, wv, slabs, stages; size_t smem; };
 
 // What a CTA has to do: batch entry, heads n0 .. n0 + hpc, columns from col0 on (of head n0)
 struct ChainWork { int b, n0, slab; };
-__device__ __forceinline__ ChainWork chain_work(const DeltaArgs &a, void *scratch) {
+template <bool PACKED> __device__ __forceinline__ ChainWork chain_work(const DeltaArgs &a, void *scratch) {
   const int slabs = a.V / (16 * a.wv), per = (a.N / a.hpc) * slabs;
   ChainWork w;
   w.b = (int)(blockIdx.x / per);
+  // sequences of a packed batch longest first: a long one that starts last keeps the others' SMs idle.  (Every CTA ranks for itself, B^2
+  // comparisons over its threads: up to 64 sequences.  Kernels of their own: the call alone costs the others 3 %.)
+  if (PACKED) w.b = __shfl_sync(0xffffffffu, a.B > 1 && a.B <= 64 ? longest_first(a.cu, a.B, w.b, static_cast<int *>(scratch)) : w.b, 0);
   const int r = (int)(blockIdx.x % per);
   w.n0 = r / slabs * a.hpc;
   w.slab = r % slabs;
@@ -286,7 +291,7 @@ __device__ __forceinline__ int chain_role(const DeltaArgs &a, int nw) {
   }                                                                                                                                           \
   begin_dependent();                                                                                                                          \
   __syncthreads();                                                                                                                            \
-  const ChainWork w = chain_work(a, smem);                                                                                                    \
+  const ChainWork w = chain_work<PACKED>(a, smem);                                                                                                    \
   const DeltaSpan sp = delta_span<C>(a, w.b);                                                                                                 \
   const uint32_t ring = smem_u32(smem), sb = (uint32_t)stage_bytes(K, nw, a.hpc);                                                             \
   if (warp > nw) return;                                                                                                                      \
@@ -301,7 +306,7 @@ __device__ __forceinline__ int chain_role(const DeltaArgs &a, int nw) {
   const size_t st_at = ((size_t)w.b * a.N + n) * K * V + v0
 
 // Y: y is asked for; KEEP: states and updates are kept for the gradient
-template <int K, bool Y, bool KEEP>
+template <int K, bool Y, bool KEEP, bool PACKED>
 __global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, int stages) {
   CHAIN_BEGIN(a.v, a.vs, false);
   const uint32_t out = ring + stages * sb + warp * out_bytes(K);
@@ -439,7 +444,7 @@ __global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, in
   if (a.hT) state_out<K>(S, a.hT, st_at, a.state_bf16, V, g, c);
 }
 
-template <int K>
+template <int K, bool PACKED>
 __global__ void __launch_bounds__(160, 2) delta_chain_bwd_kernel(DeltaArgs a, int stages) {
   CHAIN_BEGIN(a.dy, (long long)a.N * a.V, true);
   float S[K / 8][4];    // dS
@@ -552,21 +557,27 @@ ChainPlan plan_chain(const DeltaArgs &a) {
   }
   p.slabs = cols / p.wv;
   const int nw = p.hpc * p.wv;
-  // two CTAs to an SM where there are that many
-  const size_t room = (size_t)(units * p.slabs > sms ? 113 : 226) * 1024, fixed = (size_t)nw * out_bytes(a.K), sb = (size_t)stage_bytes(a.K, nw, p.hpc);
+  // Two CTAs to an SM where there are that many, but above K = 64 one: four chains of K = 128 take 1.5 us a chunk, eight 2.9, and a batch
+  // is done no sooner than its longest sequence (12 of up to 4 000 tokens, 16 heads: 370 us with two, 266 with one).
+  const bool one = a.K > 64;
+  const size_t room = (size_t)(!one && units * p.slabs > sms ? 113 : 226) * 1024, fixed = (size_t)nw * out_bytes(a.K), sb = (size_t)stage_bytes(a.K, nw, p.hpc);
   while (p.stages > 3 && fixed + p.stages * sb > room) --p.stages;
-  p.smem = fixed + p.stages * sb;
+  p.smem = std::max(fixed + p.stages * sb, one ? (size_t)115 * 1024 : 0);
   return p;
 }
 
-template <int K> cudaError_t launch_k(const DeltaArgs &args, bool backward, cudaStream_t s) {
+template <int K, bool PACKED> cudaError_t launch_kp(const DeltaArgs &args, bool backward, cudaStream_t s) {
   DeltaArgs a = args;
   const ChainPlan p = plan_chain(a);
   a.hpc = p.hpc; a.wv = p.wv; a.sms = sm_count();
-  void (*kernel)(DeltaArgs, int) = backward ? delta_chain_bwd_kernel<K> : !a.states ? delta_chain_fwd_kernel<K, true, false> : a.y ? delta_chain_fwd_kernel<K, true, true> : delta_chain_fwd_kernel<K, false, true>;
+  void (*kernel)(DeltaArgs, int) = backward ? delta_chain_bwd_kernel<K, PACKED> : !a.states ? delta_chain_fwd_kernel<K, true, false, PACKED>
+                                   : a.y ? delta_chain_fwd_kernel<K, true, true, PACKED> : delta_chain_fwd_kernel<K, false, true, PACKED>;
   const cudaError_t e = allow_smem(kernel, p.smem);
   if (e != cudaSuccess) return e;
   return launch_early(kernel, dim3((unsigned)((long long)a.B * (a.N / p.hpc) * p.slabs)), dim3(p.wv == 2 ? 128 : 32 * (p.wv + 1)), p.smem, s, a, p.stages);
+}
+template <int K> cudaError_t launch_k(const DeltaArgs &a, bool backward, cudaStream_t s) {
+  return a.cu ? launch_kp<K, true>(a, backward, s) : launch_kp<K, false>(a, backward, s);
 }
 cudaError_t launch(const DeltaArgs &a, bool backward, cudaStream_t s) {
   switch (a.K) {

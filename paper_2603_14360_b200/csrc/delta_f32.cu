@@ -24,10 +24,11 @@ __global__ void __launch_bounds__(128) delta_prep_f32_kernel(DeltaArgs a) {
   extern __shared__ __align__(16) float sm[];
   begin_dependent();
   const int K = a.K, PK = K + 4, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const long long bc = blockIdx.x / a.N;
-  const int n = (int)(blockIdx.x % a.N), b = (int)(bc / a.nch), ch = (int)(bc % a.nch);
+  const unsigned at = blockIdx.x / (unsigned)a.N;
+  const int n = (int)(blockIdx.x - at * a.N), b = a.cu ? delta_entry<C, true>(a, at) : delta_entry<C, false>(a, at);
   const DeltaSpan sp = delta_span<C>(a, b);
-  if (ch >= sp.n) return;
+  const int ch = (int)(at - sp.slot0);
+  if (ch >= sp.n) return;      // (of a packed batch: a slot that is no sequence's)
   const long long tok = sp.tok0 + ch * C;
   const int have = min(C, sp.T - ch * C);
   float *ks = sm, *qs = ks + C * PK, *Ms = qs + C * PK, *vec = Ms + C * (C + 4);
@@ -317,10 +318,11 @@ __global__ void __launch_bounds__(kThreads) delta_grad_f32_kernel(DeltaArgs a) {
   extern __shared__ __align__(16) float sm[];
   begin_dependent();
   const int K = a.K, V = a.V, PK = K + 1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const long long bc = blockIdx.x / a.N;
-  const int n = (int)(blockIdx.x % a.N), b = (int)(bc / a.nch), ch = (int)(bc % a.nch);
+  const unsigned at = blockIdx.x / (unsigned)a.N;
+  const int n = (int)(blockIdx.x - at * a.N), b = a.cu ? delta_entry<C, true>(a, at) : delta_entry<C, false>(a, at);
   const DeltaSpan sp = delta_span<C>(a, b);
-  if (ch >= sp.n) return;
+  const int ch = (int)(at - sp.slot0);
+  if (ch >= sp.n) return;      // (of a packed batch: a slot that is no sequence's)
   const long long tok = sp.tok0 + ch * C;
   const int have = min(C, sp.T - ch * C);
   const size_t slot = (size_t)(sp.slot0 + ch) * a.N + n;
@@ -523,14 +525,14 @@ template <bool BWD> cudaError_t chain(const DeltaArgs &a, cudaStream_t s) {
 
 cudaError_t launch_delta_fwd_f32(const DeltaArgs &a, cudaStream_t s) {
   const size_t smem = (size_t)(2 * C * (a.K + 4) + C * (C + 4) + 8 * C) * sizeof(float);
-  const cudaError_t e = launch_early(delta_prep_f32_kernel, dim3((unsigned)((long long)a.B * a.nch * a.N)), dim3(128), smem, s, a);
+  const cudaError_t e = launch_early(delta_prep_f32_kernel, dim3((unsigned)(a.slots * a.N)), dim3(128), smem, s, a);
   return e != cudaSuccess ? e : chain<false>(a, s);
 }
 cudaError_t launch_delta_bwd_f32(const DeltaArgs &a, cudaStream_t s) {
   cudaError_t e = chain<true>(a, s);
   const size_t smem = (size_t)grad_floats(a.K, a.V) * sizeof(float);
   if (e == cudaSuccess) e = allow_smem(delta_grad_f32_kernel, smem);
-  return e != cudaSuccess ? e : launch_early(delta_grad_f32_kernel, dim3((unsigned)((long long)a.B * a.nch * a.N)), dim3(kThreads), smem, s, a);
+  return e != cudaSuccess ? e : launch_early(delta_grad_f32_kernel, dim3((unsigned)(a.slots * a.N)), dim3(kThreads), smem, s, a);
 }
 
 }  // namespace m2rnn

@@ -69,16 +69,25 @@ __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, 
   begin_dependent();
   __syncthreads();
 
-  // the first job from number j on that there is (of a packed batch's shorter sequences some are not)
+  // the first job from number j on that there is (of a packed batch a slot may be no sequence's)
+  int entry = -1;      // the batch entry of the last one
   auto find = [&](unsigned &j) {
     GradJob o{};
     for (; j < jobs; j += gridDim.x) {
-      const unsigned bc = j / runs, run = j - bc * runs;
-      const int b = (int)(bc / (unsigned)a.nch), ch = (int)(bc - (unsigned)b * a.nch);
-      const DeltaSpan sp = delta_span<C>(a, b);
+      const unsigned slot = j / runs, run = j - slot * runs;
+      if (!a.cu) entry = delta_entry<C, false>(a, slot);
+      else if (entry < 0) entry = delta_entry<C, true>(a, slot);
+      DeltaSpan sp = delta_span<C>(a, entry);
+      while (a.cu && entry + 1 < a.B) {      // (slots only grow)
+        const DeltaSpan after = delta_span<C>(a, entry + 1);
+        if (after.slot0 > slot) break;
+        ++entry;
+        sp = after;
+      }
+      const int ch = (int)(slot - sp.slot0);
       if (ch >= sp.n) continue;
       o.tok = sp.tok0 + ch * C;
-      o.slot = (size_t)(sp.slot0 + ch) * a.N;
+      o.slot = (size_t)slot * a.N;
       o.have = min(C, sp.T - ch * C);
       o.run = (int)run;
       o.n0 = (int)run * a.hpc;
@@ -447,7 +456,7 @@ template <int K, bool MULTI, int VS> cudaError_t launch_kmv(const DeltaArgs &a, 
   const auto kernel = delta_grad_kernel<K, KG, MULTI, VS, BUFS, CTAS>;
   const cudaError_t e = allow_smem(kernel, smem);
   if (e != cudaSuccess) return e;
-  const unsigned jobs = (unsigned)((long long)a.B * a.nch * (a.N / a.hpc)), most = CTAS * (unsigned)sm_count();
+  const unsigned jobs = (unsigned)(a.slots * (a.N / a.hpc)), most = CTAS * (unsigned)sm_count();
   return launch_early(kernel, dim3(jobs < most ? jobs : most), dim3(Cfg::kThreads), smem, s, a, jobs);
 }
 template <int K, bool MULTI> cudaError_t launch_km(const DeltaArgs &a, cudaStream_t s) {

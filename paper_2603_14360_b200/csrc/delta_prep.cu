@@ -33,18 +33,17 @@ __device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], 
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-template <int K>
+template <int K, bool PACKED>
 __global__ void __launch_bounds__(32 * kWarps, 4) delta_prep_kernel(DeltaArgs a, int run) {
   __shared__ __align__(16) float sm[kWarps][kWarpFloats];
   begin_dependent();
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-  // (a packed batch's sequences are of different lengths: warps of chunks that a sequence does not have leave at once)
-  const unsigned runs = (unsigned)(a.N / run), job = blockIdx.x * kWarps + warp, bc = job / runs;
-  const int n0 = (int)(job - bc * runs) * run;
-  const int b = (int)(bc / (unsigned)a.nch), ch = (int)(bc - (unsigned)b * a.nch);
-  if (b >= a.B) return;
+  const unsigned runs = (unsigned)(a.N / run), job = blockIdx.x * kWarps + warp, slot = job / runs;
+  if (slot >= a.slots) return;
+  const int n0 = (int)(job - slot * runs) * run, b = delta_entry<kDeltaChunk, PACKED>(a, slot);
   const DeltaSpan sp = delta_span<kDeltaChunk>(a, b);
-  if (ch >= sp.n) return;
+  const int ch = PACKED ? (int)(slot - sp.slot0) : (int)(slot - (unsigned)b * a.nch);
+  if (ch >= sp.n) return;      // (of a packed batch: a slot that is no sequence's)
   const long long tok = sp.tok0 + ch * kDeltaChunk;
   const int have = min(kDeltaChunk, sp.T - ch * kDeltaChunk);
   const char *kg = static_cast<const char *>(a.k) + 2 * ((tok + g) * a.ks + (unsigned)n0 / (unsigned)a.per_k * K);
@@ -116,8 +115,8 @@ __global__ void __launch_bounds__(32 * kWarps, 4) delta_prep_kernel(DeltaArgs a,
       const float sk = __shfl_sync(0xffffffffu, g & 1 ? kk[tile][r + 1] : kk[tile][r], 4 * g + (g >> 1));
       const float sq = __shfl_sync(0xffffffffu, g & 1 ? qq[x][r + 1] : qq[x][r], 4 * g + (g >> 1));
       const bool row = 8 * x + g < have;      // (rows behind the last token: eps may be 0)
-      rki[x] = row ? rsqrtf(sk + a.eps) : 0.f;
-      rqi[x] = row ? rsqrtf(sq + a.eps) : 0.f;
+      rki[x] = rsqrtf(row ? sk + a.eps : 1.f);
+      rqi[x] = rsqrtf(row ? sq + a.eps : 1.f);
     }
     rkj[x][0] = __shfl_sync(0xffffffffu, rki[x], 8 * c);
     rkj[x][1] = __shfl_sync(0xffffffffu, rki[x], 8 * c + 4);
@@ -242,15 +241,15 @@ template <int K> cudaError_t launch_k(const DeltaArgs &a, cudaStream_t s) {
   int run = dq, o = dk;
   while (o) { const int t = run % o; run = o; o = t; }          // heads in a row that share both q and k
   // a run is cut where that makes warps for the SMs to work on
-  const long long chunks = a.cu ? a.TT / kDeltaChunk + a.B : (long long)a.B * a.nch, want = (long long)sm_count() * 8;
+  const long long want = (long long)sm_count() * 8;
   int per = run;
   for (int d = run; d >= 1; --d)
     if (run % d == 0) {
       per = d;
-      if (chunks * (a.N / d) >= want) break;
+      if (a.slots * (a.N / d) >= want) break;
     }
-  const long long jobs = (long long)a.B * a.nch * (a.N / per);
-  return launch_early(delta_prep_kernel<K>, dim3((unsigned)((jobs + kWarps - 1) / kWarps)), dim3(32 * kWarps), 0, s, a, per);
+  const long long jobs = a.slots * (a.N / per);
+  return launch_early(a.cu ? delta_prep_kernel<K, true> : delta_prep_kernel<K, false>, dim3((unsigned)((jobs + kWarps - 1) / kWarps)), dim3(32 * kWarps), 0, s, a, per);
 }
 
 }  // namespace
