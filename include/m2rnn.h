@@ -292,6 +292,9 @@ int m2rnn_conv_silu_bwd(int32_t B, int32_t T, int32_t C, int32_t io_dtype, const
  * With M2RNN_BF16 the sequence is taken in chunks of 32 tokens whose products run on tensor cores: bf16 operands (the
  * state's included), fp32 accumulation, the state itself held in fp32.  Outputs of fp32 type (a state_dtype of
  * M2RNN_F32) then carry the error of those operands, some 3e-3 of their norm.  With M2RNN_F32 everything is fp32 FMA.
+ * What is not finite stays behind its token: no y of an earlier one, of another head or sequence changes (in q: only
+ * that token's y; in v: only that column).  The gradients of a sequence with such a value, in dy or d_hT too, are
+ * undefined.
  * Supported sizes: K a multiple of 16 in 16..128, V in {16,32,64,128}. */
 typedef enum {
   M2RNN_STEP_VALUE = 0, /* step tensor IS b_t            */

@@ -25,8 +25,8 @@ enum {
   kVecG = 4, kVecRk = 5, kVecRq = 6,
   kVecDlog = 7   // d log a / d gate entry
 };
+constexpr int kRecChain = kRecVec + 4 * 128 + 128;     // what the chains read of it: up to and with kVecG
 constexpr int kRecF32Bytes = (3 * 256 + 8 * 16) * 4;   // fp32: T, P, M 16 x 16, then the vectors
-constexpr int kRecChain = kRecVec + 4 * 128 + 128;   // what the chains read of it: up to and with kVecG
 
 struct DeltaArgs {
   int B, T, N, Nq, Nk, K, V;
@@ -51,9 +51,11 @@ struct DeltaArgs {
   int nch;                     // chunks of the longest sequence
   long long slots;             // chunk slots of the batch
   int per_q, per_k;            // heads to a q head, to a k head
-  int sms;                     // chains: SMs of the device
-  int hpc, wv;                 // chains: heads and 16-column warps per head of a CTA; gradient kernel: heads of a CTA
+  int sms, nw;                 // chains: SMs of the device, 16-column warps of a CTA
+  int hpc;                     // gradient kernel: heads of a job
 };
+
+__host__ __device__ inline int delta_chunks(int T, int C) { return T / C + (T % C != 0); }
 
 // First token, length, first chunk slot and chunks of batch entry b.  Of a packed batch, sequence b's slots start at
 // cu[b] / chunk + b: no two overlap, whatever the lengths.  Offsets are cut to 0 .. TT and lengths to T: nothing is
@@ -72,7 +74,7 @@ template <int C> __device__ __forceinline__ DeltaSpan delta_span(const DeltaArgs
     s.T = a.T;
     s.slot0 = (long long)b * a.nch;
   }
-  s.n = (s.T + C - 1) / C;
+  s.n = delta_chunks(s.T, C);
   return s;
 }
 // The batch entry that chunk slot `slot` belongs to (every lane of a warp calls it): of a packed batch the last one whose slots do not start
@@ -89,7 +91,7 @@ template <int C, bool PACKED> __device__ __forceinline__ int delta_entry(const D
 }
 #endif
 inline size_t delta_slots(const m2rnn_delta_params *p, size_t tokens, int C) {
-  return p->cu_seqlens ? tokens / C + p->B : (size_t)p->B * ((p->T + C - 1) / C);
+  return p->cu_seqlens ? tokens / C + p->B : (size_t)p->B * delta_chunks(p->T, C);
 }
 
 cudaError_t launch_delta_prep(const DeltaArgs &a, cudaStream_t s);        // delta_prep.cu

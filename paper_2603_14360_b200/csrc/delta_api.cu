@@ -40,7 +40,7 @@ int check_params(const m2rnn_delta_params *p, bool step) {
     if (given[x] != 0 && (given[x] < dense[x] || given[x] % unit16)) return M2RNN_ERR_SHAPE;
   if (p->total_tokens < 0 || (!p->cu_seqlens && p->total_tokens != 0)) return M2RNN_ERR_SHAPE;
   if (p->cu_seqlens && p->total_tokens > (int64_t)p->B * p->T) return M2RNN_ERR_SHAPE;
-  if ((int64_t)p->B * ((p->T + 15) / 16 + 1) > (int64_t)0x7fffffff / p->N) return M2RNN_ERR_SHAPE;
+  if ((p->cu_seqlens ? p->total_tokens / 16 + p->B : (int64_t)p->B * (delta_chunks(p->T, 16) + 1)) > (int64_t)0x7fffffff / p->N) return M2RNN_ERR_SHAPE;
   return M2RNN_OK;
 }
 
@@ -89,7 +89,7 @@ DeltaArgs base_args(const m2rnn_delta_params *p, const void *q, const void *k, c
   a.vs = p->v_stride ? p->v_stride : (long long)p->N * p->V;
   a.TT = (long long)tokens_of(p);
   a.cu = p->cu_seqlens;
-  a.nch = (p->T + chunk_of(p) - 1) / chunk_of(p);
+  a.nch = delta_chunks(p->T, chunk_of(p));
   a.slots = (long long)delta_slots(p, tokens_of(p), chunk_of(p));
   a.per_q = p->N / p->Nq; a.per_k = p->N / p->Nk;
   return a;

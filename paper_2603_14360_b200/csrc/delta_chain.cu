@@ -1,6 +1,6 @@
 // Gated delta rule, bf16: the two chains over the chunks of a sequence, forward and backward.
 //
-// With S the K x V state at a chunk's start, T and P of delta_prep.cu, and per token the factors of DeltaVec,
+// With S the K x V state at a chunk's start, T and P of delta_prep.cu, and per token the record's factors,
 //     X = b (V - e^g K^ S)      U = T X      Y = s e^g Q^ S + P U      S' = e^g_last S + (e^(g_last - g) K^)^T U
 // and backward, from dS' at a chunk's end (K^, Q^: the rows divided by their lengths),
 //     dU = P^T dY + e^(g_last - g) K^ dS'      L = T^T dU      dV = b L
@@ -27,28 +27,28 @@ namespace {
 
 constexpr int C = kDeltaChunk;
 
-// Bytes of a stage: K, Q rows, rows of 16 nw columns of V (dY), nw / wv records
+// Bytes of a stage: K, Q rows, rows of 16 nw columns of V (dY), a record
 __host__ __device__ constexpr int pitch_k(int K) { return 2 * K + 16; }
 __host__ __device__ constexpr int pitch_v(int nw) { return 32 * nw + 16; }
-__host__ __device__ constexpr int stage_bytes(int K, int nw, int heads) { return C * (2 * pitch_k(K) + pitch_v(nw)) + heads * kRecChain; }
+__host__ __device__ constexpr int stage_bytes(int K, int nw) { return C * (2 * pitch_k(K) + pitch_v(nw)) + kRecChain; }
 
 // Forward, a chain warp's S as operands of the next chunk's pass (Y): in registers where K leaves them, else in shared memory, blocks
 // [column tile][feature tile].  (Shared memory's bandwidth is what chains of an SM compete for: 324 of its cycles a chain and chunk of K = 64.)
 __host__ __device__ constexpr int out_bytes(int K) { return K <= 64 ? 0 : 32 * K; }
 
-struct ChainPlan { int hpc, wv, slabs, stages; size_t smem; };
+struct ChainPlan { int nw, slabs, stages; size_t smem; };      // nw: 16-column warps of a CTA
 
-// What a CTA has to do: batch entry, heads n0 .. n0 + hpc, columns from col0 on (of head n0)
-struct ChainWork { int b, n0, slab; };
+// What a CTA has to do: batch entry, head, and which slab of its columns
+struct ChainWork { int b, n, slab; };
 template <bool PACKED> __device__ __forceinline__ ChainWork chain_work(const DeltaArgs &a, void *scratch) {
-  const int slabs = a.V / (16 * a.wv), per = (a.N / a.hpc) * slabs;
+  const int slabs = a.V / (16 * a.nw), per = a.N * slabs;
   ChainWork w;
   w.b = (int)(blockIdx.x / per);
   // sequences of a packed batch longest first: a long one that starts last keeps the others' SMs idle.  (Every CTA ranks for itself, B^2
   // comparisons over its threads: up to 64 sequences.  Kernels of their own: the call alone costs the others 3 %.)
   if (PACKED) w.b = __shfl_sync(0xffffffffu, a.B > 1 && a.B <= 64 ? longest_first(a.cu, a.B, w.b, static_cast<int *>(scratch)) : w.b, 0);
   const int r = (int)(blockIdx.x % per);
-  w.n0 = r / slabs * a.hpc;
+  w.n = r / slabs;
   w.slab = r % slabs;
   return w;
 }
@@ -61,15 +61,15 @@ __device__ __forceinline__ void chain_fill(const DeltaArgs &a, const ChainWork &
                                            uint64_t *full, uint64_t *empty, int lane, bool backward) {
   constexpr int P = K / 8, LR = P % 16 == 0 ? 16 : P % 8 == 0 ? 8 : P % 4 == 0 ? 4 : 2, RP = 32 / LR;      // pieces, lanes to a row; rows to a pass
   const int pv = pitch_v(nw), lv = 2 * nw, rv = 32 / lv;                                                    // of v: lanes to a row, rows to a pass
-  const uint32_t sb = (uint32_t)stage_bytes(K, nw, a.hpc);
+  const uint32_t sb = (uint32_t)stage_bytes(K, nw);
   const int r0 = lane / LR, rv0 = lane / lv;
-  const char *kp = static_cast<const char *>(a.k) + 2 * ((sp.tok0 + r0) * a.ks + w.n0 / a.per_k * K) + 16 * (lane % LR);
-  const char *qp = static_cast<const char *>(a.q) + 2 * ((sp.tok0 + r0) * a.qs + w.n0 / a.per_q * K) + 16 * (lane % LR);
-  const char *vp = static_cast<const char *>(vg) + 2 * ((sp.tok0 + rv0) * vs + (long long)w.n0 * a.V + w.slab * 16 * a.wv) + 16 * (lane % lv);
+  const char *kp = static_cast<const char *>(a.k) + 2 * ((sp.tok0 + r0) * a.ks + w.n / a.per_k * K) + 16 * (lane % LR);
+  const char *qp = static_cast<const char *>(a.q) + 2 * ((sp.tok0 + r0) * a.qs + w.n / a.per_q * K) + 16 * (lane % LR);
+  const char *vp = static_cast<const char *>(vg) + 2 * ((sp.tok0 + rv0) * vs + (long long)w.n * a.V + w.slab * 16 * nw) + 16 * (lane % lv);
   const long long kc = 2 * C * a.ks, qc = 2 * C * a.qs, vc = 2 * C * vs, kr = 2 * RP * a.ks, qr = 2 * RP * a.qs, vr = 2 * rv * vs;      // bytes to the next chunk, the next pass
   const uint32_t k_at = r0 * pitch_k(K) + 16 * (lane % LR), v_at = 2 * C * pitch_k(K) + rv0 * pv + 16 * (lane % lv);
   const size_t rec_step = (size_t)a.N * kRecBytes;
-  const char *rp = a.rec + ((size_t)sp.slot0 * a.N + w.n0) * kRecBytes;
+  const char *rp = a.rec + ((size_t)sp.slot0 * a.N + w.n) * kRecBytes;
   if (backward) {
     kp += (sp.n - 1) * kc; qp += (sp.n - 1) * qc; vp += (sp.n - 1) * vc; rp += (sp.n - 1) * rec_step;
   }
@@ -84,8 +84,8 @@ __device__ __forceinline__ void chain_fill(const DeltaArgs &a, const ChainWork &
     }
     const uint32_t base = ring + st * sb, kd = base + k_at, vd = base + v_at, rd = base + C * (2 * pitch_k(K) + pv);
     if (lane == 0) {
-      mbar_expect(full + st, (uint32_t)(a.hpc * kRecChain));
-      for (int h = 0; h < a.hpc; ++h) bulk_load(rd + h * kRecChain, rp + (size_t)h * kRecBytes, kRecChain, full + st);
+      mbar_expect(full + st, (uint32_t)kRecChain);
+      bulk_load(rd, rp, kRecChain, full + st);
     }
     const char *ks = kp, *qs = qp, *vv = vp;
     if (have == C) {
@@ -233,6 +233,39 @@ __device__ __forceinline__ void mul_lower(float (&acc)[4][4], const uint32_t (&A
   mma_add(acc[0], A[1], b[1][0], b[1][1]);
   mma_add(acc[1], A[1], b[1][2], b[1][3]);
 }
+// Causality and what is not finite: in a product with a lower triangular matrix 0 x NaN would carry a token's NaN to the tokens before it, of
+// its block of 16.  Where U has such entries they are taken out of the operands, and per column the first such token is kept; from that one on
+// results are NaN.
+__device__ __forceinline__ bool any_odd(const uint32_t (&f)[2][4]) {
+  __nv_bfloat162 s = __floats2bfloat162_rn(0.f, 0.f), t = s;
+  const __nv_bfloat162 z = s;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    s = __hfma2(reinterpret_cast<const __nv_bfloat162 &>(f[0][r]), z, s);
+    t = __hfma2(reinterpret_cast<const __nv_bfloat162 &>(f[1][r]), z, t);
+  }
+  s = __hadd2(s, t);
+  return __any_sync(0xffffffffu, (reinterpret_cast<const uint32_t &>(s) & 0x7fff7fffu) != 0u);
+}
+struct FirstOdd { int at[2]; };      // of columns g, g + 8; 32: none
+__device__ __forceinline__ FirstOdd take_odd(uint32_t (&f)[2][4], int c) {
+  FirstOdd o{{32, 32}};
+#pragma unroll
+  for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if ((f[kt][r] >> (16 * e) & 0x7f80u) == 0x7f80u) {
+          f[kt][r] &= e ? 0xffffu : 0xffff0000u;
+          o.at[r & 1] = min(o.at[r & 1], 16 * kt + 8 * (r >> 1) + 2 * c + e);
+        }
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int d = 1; d < 4; d *= 2) o.at[h] = min(o.at[h], __shfl_xor_sync(0xffffffffu, o.at[h], d));
+  return o;
+}
 __device__ __forceinline__ void zero(float (&x)[4][4]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -284,24 +317,24 @@ __device__ __forceinline__ int chain_role(const DeltaArgs &a, int nw) {
 #define CHAIN_BEGIN(tensor, stride, back)                                                                                                     \
   extern __shared__ __align__(128) unsigned char smem[];                                                                                      \
   __shared__ ChainBars bars;                                                                                                                  \
-  const int nw = a.hpc * a.wv, warp = chain_role(a, nw), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;                                 \
+  const int nw = a.nw, warp = chain_role(a, nw), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;                                         \
   if (threadIdx.x == 0) {                                                                                                                     \
     for (int i = 0; i < stages; ++i) { mbar_init(bars.full + i, 33); mbar_init(bars.empty + i, nw); }                                         \
     fence_mbar_init();                                                                                                                        \
   }                                                                                                                                           \
   begin_dependent();                                                                                                                          \
   __syncthreads();                                                                                                                            \
-  const ChainWork w = chain_work<PACKED>(a, smem);                                                                                                    \
+  const ChainWork w = chain_work<PACKED>(a, smem);                                                                                            \
   const DeltaSpan sp = delta_span<C>(a, w.b);                                                                                                 \
-  const uint32_t ring = smem_u32(smem), sb = (uint32_t)stage_bytes(K, nw, a.hpc);                                                             \
+  const uint32_t ring = smem_u32(smem), sb = (uint32_t)stage_bytes(K, nw);                                                                    \
   if (warp > nw) return;                                                                                                                      \
   if (warp == nw) {                                                                                                                           \
     chain_fill<K>(a, w, sp, tensor, stride, nw, stages, ring, bars.full, bars.empty, lane, back);                                             \
     return;                                                                                                                                   \
   }                                                                                                                                           \
-  const int n = w.n0 + warp / a.wv, v0 = 16 * (w.slab * a.wv + warp % a.wv), V = a.V, pv = pitch_v(nw);                                        \
+  const int n = w.n, v0 = 16 * (w.slab * nw + warp), V = a.V, pv = pitch_v(nw);                                                               \
   const Lanes l(lane);                                                                                                                        \
-  const uint32_t v_off = 2 * C * pitch_k(K), r_off = v_off + C * pv + (warp / a.wv) * kRecChain;                                               \
+  const uint32_t v_off = 2 * C * pitch_k(K), r_off = v_off + C * pv;                                                                          \
   const uint32_t v_at = v_off + 32 * warp + (l.row + 8 * l.mat_hi) * pv + 16 * l.mat_lo, v_mine = v_off + 32 * warp + lane * pv;                \
   const size_t st_at = ((size_t)w.b * a.N + n) * K * V + v0
 
@@ -309,7 +342,7 @@ __device__ __forceinline__ int chain_role(const DeltaArgs &a, int nw) {
 template <int K, bool Y, bool KEEP, bool PACKED>
 __global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, int stages) {
   CHAIN_BEGIN(a.v, a.vs, false);
-  const uint32_t out = ring + stages * sb + warp * out_bytes(K);
+  const uint32_t out = ring + stages * sb + warp * out_bytes(K), spare = ring + stages * sb + nw * out_bytes(K) - v_off;      // (spare: as if a stage, its columns of V)
   float S[K / 8][4];
   if (a.h0) state_in<K>(S, a.h0, st_at, a.state_bf16, V, g, c);
   else
@@ -333,6 +366,56 @@ __global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, in
     }
     mul_lower_t(y, Ub, P);
   };
+  // X from K S, as operands; T
+  auto x_of = [&](uint32_t stage, float (&acc)[4][4], uint32_t (&A)[2][4], uint32_t (&T)[3][4]) {
+    const uint32_t vec = stage + r_off + kRecVec + 8 * c;
+    uint32_t vt[2][4];
+    rows_in(vt, stage + v_at, pv);
+    lower_t_in(T, stage + r_off + kRecT, l);
+#pragma unroll
+    for (int nt = 0; nt < 4; ++nt) {
+      const float2 e = lds64(vec + 128 * kVecEgk + 32 * nt), b = lds64(vec + 128 * kVecBeta + 32 * nt);
+      const float2 x0 = unpack_bf16(vt[nt >> 1][2 * (nt & 1)]), x1 = unpack_bf16(vt[nt >> 1][2 * (nt & 1) + 1]);
+      acc[nt][0] = b.x * fmaf(-e.x, acc[nt][0], x0.x);
+      acc[nt][1] = b.y * fmaf(-e.y, acc[nt][1], x0.y);
+      acc[nt][2] = b.x * fmaf(-e.x, acc[nt][2], x1.x);
+      acc[nt][3] = b.y * fmaf(-e.y, acc[nt][3], x1.y);
+    }
+    pack_a<4>(acc, 0, A[0]);
+    pack_a<4>(acc, 1, A[1]);
+  };
+  // Where a chunk's U has what is not finite, before its Y: U once more from the S that Y is going to read, and y begun with NaN from the first
+  // such token on.
+  bool odd = false;
+  auto mend = [&](uint32_t stage) {
+    RowsT<K> kb;
+    kb.start(stage, l);
+    float acc[4][4], U[4][4];
+    zero(acc);
+#pragma unroll
+    for (int kt = 0; kt < K / 16; ++kt) {
+      if constexpr (K > 64) {
+        uint32_t f[4];
+        ldmatrix_x4(s_at + 256 * kt, f);
+        kb.step(acc, f, kt);
+      } else {
+        kb.step(acc, Sb[kt], kt);
+      }
+    }
+    uint32_t A[2][4], T[3][4];
+    x_of(stage, acc, A, T);
+    const FirstOdd x = take_odd(A, c);
+    zero(U);
+    mul_lower_t(U, A, T);
+    pack_a<4>(U, 0, Ub[0]);
+    pack_a<4>(U, 1, Ub[1]);
+    const FirstOdd u = take_odd(Ub, c);      // (T's rows may have such entries where X has none)
+#pragma unroll
+    for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (8 * nt + 2 * c + (r & 1) >= min(x.at[r >> 1], u.at[r >> 1])) y[nt][r] = __int_as_float(0x7fffffff);
+  };
   // One pass works on a chunk's chain and on the chunk before's Y.  (The first pass's Y is made of what there is, and not stored.)
   int st = 0, before = 0;
   uint32_t phase = 0;
@@ -343,13 +426,14 @@ __global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, in
       return;
     }
     const uint32_t stage = ring + st * sb, last = ring + before * sb, vec = stage + r_off + kRecVec + 8 * c;
+    zero(y);
+    if (Y && odd) mend(last);
     RowsT<K> kb, qb;
     kb.start(stage, l);
     if (Y) qb.start(last + C * pitch_k(K), l);
     const float ec = __expf(lds32(stage + r_off + kRecVec + 128 * kVecG + 124));
     float acc[4][4];
     zero(acc);
-    zero(y);
     uint32_t fo[2][4];      // the chunk before's S
     if (Y && K > 64) ldmatrix_x4(s_at, fo[0]);
 #pragma unroll
@@ -375,22 +459,8 @@ __global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, in
       }
     }
     if (Y) y_rest(last);
-    // X
-    uint32_t vt[2][4], T[3][4];
-    rows_in(vt, stage + v_at, pv);
-    lower_t_in(T, stage + r_off + kRecT, l);
-#pragma unroll
-    for (int nt = 0; nt < 4; ++nt) {
-      const float2 e = lds64(vec + 128 * kVecEgk + 32 * nt), b = lds64(vec + 128 * kVecBeta + 32 * nt);
-      const float2 x0 = unpack_bf16(vt[nt >> 1][2 * (nt & 1)]), x1 = unpack_bf16(vt[nt >> 1][2 * (nt & 1) + 1]);
-      acc[nt][0] = b.x * fmaf(-e.x, acc[nt][0], x0.x);
-      acc[nt][1] = b.y * fmaf(-e.y, acc[nt][1], x0.y);
-      acc[nt][2] = b.x * fmaf(-e.x, acc[nt][2], x1.x);
-      acc[nt][3] = b.y * fmaf(-e.y, acc[nt][3], x1.y);
-    }
-    uint32_t A[2][4];
-    pack_a<4>(acc, 0, A[0]);
-    pack_a<4>(acc, 1, A[1]);
+    uint32_t A[2][4], T[3][4];
+    x_of(stage, acc, A, T);
     float U[4][4];
     zero(U);
     mul_lower_t(U, A, T);
@@ -413,7 +483,9 @@ __global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, in
     // S'
     rb.run(S, A);
     if (Y) {
-      rows_out(y, last + v_at, last + v_mine, pv, yg, ch > 0);      // (through V's place, which has been read)
+      odd = any_odd(Ub);
+      const uint32_t y_to = ch > 0 ? last : spare;      // (through V's place, which has been read)
+      rows_out(y, y_to + v_at, y_to + v_mine, pv, yg, ch > 0);
       if (ch > 0) yg += (size_t)C * a.N * V;
     }
     __syncwarp();
@@ -425,9 +497,10 @@ __global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, in
   }
   if (Y && sp.n > 0) {
     const uint32_t last = ring + before * sb;
+    zero(y);
+    if (odd) mend(last);
     RowsT<K> qb;
     qb.start(last + C * pitch_k(K), l);
-    zero(y);
 #pragma unroll
     for (int kt = 0; kt < K / 16; ++kt) {
       if constexpr (K > 64) {
@@ -549,18 +622,17 @@ __global__ void __launch_bounds__(160, 2) delta_chain_bwd_kernel(DeltaArgs a, in
 ChainPlan plan_chain(const DeltaArgs &a) {
   const int cols = a.V / 16;
   const long long units = (long long)a.B * a.N, sms = sm_count();
-  ChainPlan p{1, 1, 1, 4, 0};
+  ChainPlan p{1, 1, 4, 0};
   long long least = 0;
-  for (int wv = cols < 4 ? cols : 4; wv >= 1; wv /= 2) {
-    const long long chains = (units * (cols / wv) + sms - 1) / sms * wv;
-    if (!least || 4 * chains <= 3 * least) { least = chains; p.wv = wv; }
+  for (int nw = cols < 4 ? cols : 4; nw >= 1; nw /= 2) {
+    const long long chains = (units * (cols / nw) + sms - 1) / sms * nw;
+    if (!least || 4 * chains <= 3 * least) { least = chains; p.nw = nw; }
   }
-  p.slabs = cols / p.wv;
-  const int nw = p.hpc * p.wv;
+  p.slabs = cols / p.nw;
   // Two CTAs to an SM where there are that many, but above K = 64 one: four chains of K = 128 take 1.5 us a chunk, eight 2.9, and a batch
   // is done no sooner than its longest sequence (12 of up to 4 000 tokens, 16 heads: 370 us with two, 266 with one).
   const bool one = a.K > 64;
-  const size_t room = (size_t)(!one && units * p.slabs > sms ? 113 : 226) * 1024, fixed = (size_t)nw * out_bytes(a.K), sb = (size_t)stage_bytes(a.K, nw, p.hpc);
+  const size_t room = (size_t)(!one && units * p.slabs > sms ? 113 : 226) * 1024, fixed = (size_t)p.nw * out_bytes(a.K) + C * pitch_v(p.nw), sb = (size_t)stage_bytes(a.K, p.nw);
   while (p.stages > 3 && fixed + p.stages * sb > room) --p.stages;
   p.smem = std::max(fixed + p.stages * sb, one ? (size_t)115 * 1024 : 0);
   return p;
@@ -569,12 +641,12 @@ ChainPlan plan_chain(const DeltaArgs &a) {
 template <int K, bool PACKED> cudaError_t launch_kp(const DeltaArgs &args, bool backward, cudaStream_t s) {
   DeltaArgs a = args;
   const ChainPlan p = plan_chain(a);
-  a.hpc = p.hpc; a.wv = p.wv; a.sms = sm_count();
+  a.nw = p.nw; a.sms = sm_count();
   void (*kernel)(DeltaArgs, int) = backward ? delta_chain_bwd_kernel<K, PACKED> : !a.states ? delta_chain_fwd_kernel<K, true, false, PACKED>
                                    : a.y ? delta_chain_fwd_kernel<K, true, true, PACKED> : delta_chain_fwd_kernel<K, false, true, PACKED>;
   const cudaError_t e = allow_smem(kernel, p.smem);
   if (e != cudaSuccess) return e;
-  return launch_early(kernel, dim3((unsigned)((long long)a.B * (a.N / p.hpc) * p.slabs)), dim3(p.wv == 2 ? 128 : 32 * (p.wv + 1)), p.smem, s, a, p.stages);
+  return launch_early(kernel, dim3((unsigned)((long long)a.B * a.N * p.slabs)), dim3(p.nw == 2 ? 128 : 32 * (p.nw + 1)), p.smem, s, a, p.stages);
 }
 template <int K> cudaError_t launch_k(const DeltaArgs &a, bool backward, cudaStream_t s) {
   return a.cu ? launch_kp<K, true>(a, backward, s) : launch_kp<K, false>(a, backward, s);

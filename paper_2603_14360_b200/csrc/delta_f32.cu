@@ -262,6 +262,7 @@ __global__ void __launch_bounds__(288) delta_chain_f32_kernel(DeltaArgs a, int n
       for (int j = 0; j < C; ++j) u = fmaf(T[j], __shfl_sync(0xffffffffu, x, base + j), u);      // (T_lj = 0 for j > l)
       float y = 0.f;
       if (a.y) y = vec[C * kVecEq + l] * dots<M>(qs, K, S, l);
+      const float qS = y;
 #pragma unroll
       for (int m = 0; m < M; ++m) S[m] *= ec;
 #pragma unroll
@@ -272,6 +273,19 @@ __global__ void __launch_bounds__(288) delta_chain_f32_kernel(DeltaArgs a, int n
         rows_of<M>(ks + j * K + M * l, k);
 #pragma unroll
         for (int m = 0; m < M; ++m) S[m] = fmaf(k[m], e, S[m]);
+      }
+      // 0 x NaN above carried a token's NaN to the tokens before it: y without them.  (S has it in the whole column either way.)
+      if (__any_sync(0xffffffffu, !(fabsf(u) < __int_as_float(0x7f800000)))) {
+        u = 0.f;
+        y = qS;
+        for (int j = 0; j < C; ++j) {
+          const float xj = __shfl_sync(0xffffffffu, x, base + j);
+          if (j <= l) u = fmaf(rec[l * kPM + j], xj, u);
+        }
+        for (int j = 0; j < C; ++j) {
+          const float uj = __shfl_sync(0xffffffffu, u, base + j);
+          if (j <= l) y = fmaf(rec[kSP + l * kPM + j], uj, y);
+        }
       }
       if (a.y && l < have) static_cast<float *>(a.y)[((size_t)(tok + l) * a.N + n) * V + v] = y;
       if (a.upd) reinterpret_cast<float *>(a.upd)[slot * C * V + l * V + v] = u;

@@ -163,6 +163,7 @@ __global__ void __launch_bounds__(32 * kWarps, 4) delta_prep_kernel(DeltaArgs a,
       bi[x] = __shfl_sync(0xffffffffu, bt, g + 8 * x) * rki[x];
     }
     uint32_t *Pg = reinterpret_cast<uint32_t *>(rec + kRecP) + lane;
+    float odd = 0.f;      // NaN where M_21 has what is not finite
 #pragma unroll
     for (int nt = 0; nt < 4; ++nt) {
       const float g0 = __shfl_sync(0xffffffffu, gs, 8 * nt + 2 * c), g1 = __shfl_sync(0xffffffffu, gs, 8 * nt + 2 * c + 1);
@@ -172,12 +173,16 @@ __global__ void __launch_bounds__(32 * kWarps, 4) delta_prep_kernel(DeltaArgs a,
         const int tile = mt ? 2 + nt : nt;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int x = 2 * mt + h, i = g + 8 * x;      // (blocks below the diagonal are whole, those above it nothing)
-          const bool w0 = x > nt || (x == nt && i >= j), w1 = x > nt || (x == nt && i > j);
-          const float e0 = w0 ? __expf(gi[x] - g0) * rkj[nt][0] : 0.f, e1 = w1 ? __expf(gi[x] - g1) * rkj[nt][1] : 0.f;
-          const float m0 = x > nt || i > j ? bi[x] * e0 * kk[tile][2 * h] : 0.f, m1 = x > nt || i > j + 1 ? bi[x] * e1 * kk[tile][2 * h + 1] : 0.f;
-          sts64(Msa + 4u * (i * kPM + j), make_float2(m0, m1));
-          Pg[(4 * x + nt) * 32] = pack_bf16(rqi[x] * e0 * qk[tile][2 * h], rqi[x] * e1 * qk[tile][2 * h + 1]);
+          const int x = 2 * mt + h, i = g + 8 * x;      // (8 x 8 blocks below the diagonal are whole, those above it zeros)
+          uint32_t p = 0u;
+          if (x >= nt) {
+            const float e0 = __expf(gi[x] - g0) * rkj[nt][0], e1 = __expf(gi[x] - g1) * rkj[nt][1];
+            const float m0 = x > nt || i > j ? bi[x] * e0 * kk[tile][2 * h] : 0.f, m1 = x > nt || i > j + 1 ? bi[x] * e1 * kk[tile][2 * h + 1] : 0.f;
+            sts64(Msa + 4u * (i * kPM + j), make_float2(m0, m1));
+            if (x > 1 && nt < 2) odd = fmaf(0.f, m0, fmaf(0.f, m1, odd));
+            p = pack_bf16(x > nt || i >= j ? rqi[x] * e0 * qk[tile][2 * h] : 0.f, x > nt || i > j ? rqi[x] * e1 * qk[tile][2 * h + 1] : 0.f);
+          }
+          Pg[(4 * x + nt) * 32] = p;
         }
       }
     }
@@ -226,6 +231,21 @@ __global__ void __launch_bounds__(32 * kWarps, 4) delta_prep_kernel(DeltaArgs a,
       const uint32_t A[4] = {tf32(-W[kt][0]), tf32(-W[kt][2]), tf32(-W[kt][1]), tf32(-W[kt][3])};
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt) mma_tf32(Z[nt], A, tf32(t[8 * nt]), tf32(t[kPT + 8 * nt]));
+    }
+    if (__any_sync(0xffffffffu, odd != 0.f)) {      // (0 x NaN: the products would carry a token's NaN to rows before it.  By substitution, T_21 taking M_21's place.)
+#pragma unroll 1
+      for (int i = 16; i < 32; ++i) {
+        const int j = lane & 15;
+        float s = 0.f;
+        for (int m = 0; m < i; ++m) s = fmaf(-M[i * kPM + m], m < 16 ? Td[m * kPT + j] : M[m * kPM + j], s);
+        __syncwarp();
+        if (lane < 16) M[i * kPM + j] = s;
+        __syncwarp();
+      }
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) Z[nt][r] = M[(16 + g + 8 * (r >> 1)) * kPM + 8 * nt + 2 * c + (r & 1)];
     }
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt) {

@@ -93,6 +93,19 @@ def test_workspaces(lib, io):
     assert lib.m2rnn_delta_ckpt_bytes(ctypes.byref(packed)) < lib.m2rnn_delta_ckpt_bytes(ctypes.byref(par(io_dtype=io, B=50, T=4096))) / 10
 
 
+def test_longest_length(lib):
+    """A packed batch may give any upper bound of its lengths, the largest number too: sizes follow its tokens."""
+    most = (1 << 31) - 1
+    for io in (0, 1):
+        sizes = [lib.m2rnn_delta_ckpt_bytes(ctypes.byref(par(io_dtype=io, B=3, N=64, T=T, Nq=64, Nk=64, cu_seqlens=0x10000, total_tokens=5000))) for T in (5000, most)]
+        assert sizes[0] == sizes[1] > 0
+        # a dense one of that length: 2^31 tokens of 1 head, 5 120 (3 584) bytes of record to a chunk
+        p = par(io_dtype=io, B=1, N=1, Nq=1, Nk=1, K=16, V=16, T=most)
+        assert lib.m2rnn_delta_ckpt_bytes(ctypes.byref(p)) > (1 << 31) / 32 * 5120
+        assert fwd(lib, p, size=1 << 20) == -5
+    assert fwd(lib, par(T=most, N=64, Nq=64, Nk=64)) == -2
+
+
 def test_decoding_step(lib):
     assert step(lib, par(), n_slots=3) == -2                    # without slots a state for every row
     assert step(lib, par(), n_slots=-1, slots=FAKE) == -2

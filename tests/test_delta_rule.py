@@ -241,6 +241,37 @@ def test_rows_that_are_not_finite_stay_with_their_sequence(dtype):
     assert torch.isfinite(y[:70]).all() and torch.isfinite(hT).all()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("K,V", [(48, 32), (128, 64)])
+@pytest.mark.parametrize("value", [math.nan, math.inf], ids=["nan", "inf"])
+@pytest.mark.parametrize("at", [0, 3, 14, 21, 30, 47, 72])
+def test_values_that_are_not_finite_reach_no_earlier_token(dtype, K, V, value, at):
+    """As behind the last token of a right-padded batch: tokens before, other heads and other entries have the y that they had."""
+    x, on, H0, dy, d_hT, o = make(15, B=2, T=75, N=4, K=K, V=V, Nq=2, Nk=2, dtype=dtype, gate="log", step="value")
+    o = on_gpu(o)
+    want = m.m2rnn_delta_fwd(*on, H0.cuda(), **o)[0]
+    for which in range(5):
+        # what it is planted in, and the heads that it may reach (q, k: head 0's group)
+        bad = [t.clone() for t in on]
+        bad[which][(0, at, 0) if which > 2 else (0, at, 0, 5)] = value
+        heads = [0] if which > 1 else [0, 1]
+        for save in (False, True):
+            y, hT, _ = m.m2rnn_delta_fwd(*bad, H0.cuda(), save_ckpt=save, **o)
+            others = [n for n in range(4) if n not in heads]
+            assert torch.equal(y[1], want[1]) and torch.equal(y[0][:, others], want[0][:, others])
+            assert torch.isfinite(hT[1]).all() and torch.isfinite(hT[0, others]).all()
+            if at:
+                assert rel(y[0, :at], want[0, :at].cpu()) <= TOL[dtype], which
+            if which == 0:
+                assert torch.isfinite(hT).all() and torch.equal(y[0, at + 1:], want[0, at + 1:]) and not torch.isfinite(y[0, at, heads]).any()
+            elif which == 2:      # a column of the state
+                rest = [v for v in range(V) if v != 5]
+                assert not torch.isfinite(y[0, at:, 0, 5]).any() and not torch.isfinite(hT[0, 0, :, 5]).any()
+                assert torch.equal(y[0][..., rest], want[0][..., rest]) and torch.isfinite(hT[0, 0][:, rest]).all()
+            elif which != 3 or value != math.inf:      # (a decay of e^inf: by the formula, not asked for)
+                assert not torch.isfinite(y[0, at:, heads]).any() and not torch.isfinite(hT[0, heads]).any()
+
+
 def test_empty_calls():
     q = torch.zeros(2, 0, 2, 16, dtype=BF, device="cuda")
     v, gt = torch.zeros(2, 0, 2, 16, dtype=BF, device="cuda"), torch.zeros(2, 0, 2, dtype=BF, device="cuda")
