@@ -12,6 +12,7 @@
 
 #include <ATen/core/TensorBody.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <ATen/ops/from_blob.h>
 #include <ATen/ops/zeros.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGuard.h>
@@ -155,7 +156,29 @@ Tensor status_word_of(int idx) {
   std::lock_guard<std::mutex> lock(g_status_mutex);
   auto &v = status_words();
   if ((int)v.size() <= idx) v.resize(idx + 1);
-  if (!v[idx].defined()) v[idx] = at::zeros({1}, at::TensorOptions().dtype(at::kInt).device(at::kCUDA, idx));
+  if (!v[idx].defined()) {
+    const auto options = at::TensorOptions().dtype(at::kInt).device(at::kCUDA, idx);
+    const c10::cuda::CUDAGuard device((c10::DeviceIndex)idx);
+    const cudaStream_t now = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)idx).stream();
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(now, &capture) != cudaSuccess) (void)cudaGetLastError();
+    if (capture == cudaStreamCaptureStatusNone) {
+      v[idx] = at::zeros({1}, options);
+    } else {      // a device's first call, captured: the word is not the graph's, nor is it cleared whenever that is replayed
+      cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+      void *word = nullptr;
+      cudaStream_t s = nullptr;
+      cudaThreadExchangeStreamCaptureMode(&mode);
+      cudaError_t e = cudaMalloc(&word, sizeof(int32_t));
+      if (e == cudaSuccess) e = cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking);
+      if (e == cudaSuccess) e = cudaMemsetAsync(word, 0, sizeof(int32_t), s);
+      if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+      if (s) cudaStreamDestroy(s);
+      cudaThreadExchangeStreamCaptureMode(&mode);
+      if (e != cudaSuccess) fail(PyExc_RuntimeError, "status word: %s", cudaGetErrorString(e));
+      v[idx] = at::from_blob(word, {1}, options);
+    }
+  }
   return v[idx];
 }
 int32_t *status_ptr(int idx) {
@@ -169,15 +192,18 @@ int32_t *status_ptr(int idx) {
 int32_t *status_of(const Tensor &t) { return status_ptr(t.device().index()); }
 
 // Elements between consecutive tokens of q, k or v ([B,T,heads,dim] or packed [tokens,heads,dim]);
-// 0 stands for the dense layout
+// 0 stands for the dense layout.  The stride of an axis of one entry means nothing.
 int64_t token_stride(const Tensor &t, const char *name) {
   if (t.numel() == 0) return 0;
   const auto sz = t.sizes(), st = t.strides();
   const size_t d = sz.size();
-  if (st[d - 1] != 1 || st[d - 2] != sz[d - 1]) fail(PyExc_ValueError, "%s: the heads of a token must be contiguous", name);
-  const int64_t tok = st[d - 3];
-  if (d == 4 && sz[0] > 1 && st[0] != sz[1] * tok)
+  if ((sz[d - 1] > 1 && st[d - 1] != 1) || (sz[d - 2] > 1 && st[d - 2] != sz[d - 1])) fail(PyExc_ValueError, "%s: the heads of a token must be contiguous", name);
+  const bool batch = d == 4 && sz[0] > 1;
+  if (!batch && sz[d - 3] == 1) return 0;      // one token
+  const int64_t tok = batch && sz[1] == 1 ? st[0] : st[d - 3];
+  if (batch && sz[1] > 1 && st[0] != sz[1] * tok)
     fail(PyExc_ValueError, "%s: batch entries must follow one another along the token axis", name);
+  if (tok == 0) fail(PyExc_ValueError, "%s: its tokens are one and the same in memory (expanded)", name);
   return tok == sz[d - 2] * sz[d - 1] ? 0 : tok;
 }
 
@@ -212,9 +238,11 @@ Scan scan_params(const Tensor &q, const Tensor &k, const Tensor &v, long gate_ki
     p.B = (int32_t)(cu->numel() - 1);
     PyObject *n = PyNumber_Long(max_seqlen);
     if (!n) throw python_error();
-    p.T = (int32_t)PyLong_AsLong(n);
+    const long most = PyLong_AsLong(n);
     Py_DECREF(n);
     if (PyErr_Occurred()) throw python_error();
+    if (most > INT32_MAX) fail(PyExc_ValueError, "max_seqlen %ld: at most %ld", most, (long)INT32_MAX);
+    p.T = (int32_t)most;
     p.cu_seqlens = static_cast<const int32_t *>(cu->data_ptr());
     s.lead[0] = q.size(0); s.nlead = 1;
   } else {

@@ -136,6 +136,54 @@ def test_rows_behind_a_packed_batch_are_left_alone():
         assert (t[90:] == 3).all() and not (t[:90] == 3).all()
 
 
+@pytest.mark.parametrize("dtype", [BF, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("B", [1, 3])
+def test_one_token_each_as_slices_of_a_projection(dtype, B):
+    """An axis of one entry may have any stride: what a program's own operations leave there is not looked at."""
+    x, dy = inputs(10, B=B, T=1, dtype=dtype)
+    want = train(x, dy)
+    wide = torch.cat([t.flatten(2) for t in x[:3]] + [torch.zeros(B, 1, 8, device="cuda", dtype=dtype)], 2)
+    W = wide.shape[2]
+    sizes = [t[0].numel() for t in x[:3]]
+    for token in (W, 1, 7, sizes[0]):
+        odd, at = [], 0
+        for t, n in zip(x[:3], sizes):
+            odd.append(torch.as_strided(wide, t.shape, (W, token, t.shape[3], 1), at))
+            at += n
+        assert all(torch.equal(a, b) for a, b in zip(odd, x))
+        assert all(torch.equal(a, b) for a, b in zip(train(odd + x[3:], dy), want)), token
+    one_head = [t[:, :, :1] for t in x[:2]] + x[2:]      # a single q and k head, sliced out of four
+    dense = [t.contiguous() for t in one_head]
+    assert all(torch.equal(a, b) for a, b in zip(train(one_head, dy), train(dense, dy)))
+
+
+def test_first_call_captured():
+    """In a process of its own: the status word that the first call makes is not the graph's."""
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2603_14360_b200 import binding as m
+x = [torch.randn(2, 70, 2, 32, device="cuda").bfloat16() for _ in range(3)] + [-torch.rand(2, 70, 2, device="cuda").bfloat16() for _ in range(2)]
+g = torch.cuda.CUDAGraph()
+side = torch.cuda.Stream()
+side.wait_stream(torch.cuda.current_stream())
+with torch.cuda.stream(side), torch.cuda.graph(g, stream=side):
+    y = m.m2rnn_delta_fwd(*x)[0]
+assert m.device_status_word().item() == 0
+for _ in range(2):
+    m.device_status_word().fill_(5)
+    g.replay()
+    torch.cuda.synchronize()
+    assert m.device_status_word().item() == 5
+m.device_status_word().zero_()
+assert torch.equal(y, m.m2rnn_delta_fwd(*x)[0]) and torch.isfinite(y).all()
+print("fine")
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "fine" in r.stdout, r.stderr
+
+
 def test_refusals():
     x, dy = inputs(8)
     q, k, v, gate, step = x
@@ -144,6 +192,14 @@ def test_refusals():
                 (q.cpu(), k, v, gate, step)):
         with pytest.raises((ValueError, TypeError)):
             m.m2rnn_delta_fwd(*bad, **OPT)
+    for which in range(3):                                               # one token's memory for all: no layout of the calls
+        same = list(x)
+        same[which] = x[which][:1, :1].expand(2, 150, -1, -1)
+        with pytest.raises(ValueError):
+            m.m2rnn_delta_fwd(*same, **OPT)
+    flat, cu = [t.flatten(0, 1) for t in x], torch.tensor([0, 150, 300], dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        m.m2rnn_delta_fwd(*flat, cu_seqlens=cu, max_seqlen=(1 << 32) + 5, **OPT)
     with pytest.raises(m.M2RNNError):
         m.m2rnn_delta_fwd(*x, gate_kind=m.GATE_VALUE)
     with pytest.raises(m.M2RNNError):
