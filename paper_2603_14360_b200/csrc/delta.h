@@ -52,7 +52,7 @@ struct DeltaArgs {
   long long slots;             // chunk slots of the batch
   int per_q, per_k;            // heads to a q head, to a k head
   int sms, nw;                 // chains: SMs of the device, 16-column warps of a CTA
-  int hpc;                     // gradient kernel: heads of a job
+  int hpc, grad_ctas;          // gradient kernel: heads of a job, CTAs to an SM
 };
 
 __host__ __device__ inline int delta_chunks(int T, int C) { return T / C + (T % C != 0); }
@@ -97,7 +97,8 @@ inline size_t delta_slots(const m2rnn_delta_params *p, size_t tokens, int C) {
 cudaError_t launch_delta_prep(const DeltaArgs &a, cudaStream_t s);        // delta_prep.cu
 cudaError_t launch_delta_chain_fwd(const DeltaArgs &a, cudaStream_t s);   // delta_chain.cu
 cudaError_t launch_delta_chain_bwd(const DeltaArgs &a, cudaStream_t s);
-int delta_grad_heads(const m2rnn_delta_params *p, size_t slots);          // delta_grad.cu: heads of a CTA
+struct GradPlan { int heads, ctas; };
+GradPlan delta_grad_plan(const m2rnn_delta_params *p, size_t slots);      // delta_grad.cu
 cudaError_t launch_delta_grad(const DeltaArgs &a, cudaStream_t s);
 cudaError_t launch_delta_fwd_f32(const DeltaArgs &a, cudaStream_t s);     // delta_f32.cu
 cudaError_t launch_delta_bwd_f32(const DeltaArgs &a, cudaStream_t s);

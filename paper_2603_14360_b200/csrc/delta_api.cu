@@ -57,22 +57,23 @@ Ckpt ckpt_layout(const m2rnn_delta_params *p) {
   return c;
 }
 
-struct Workspace { size_t ckpt, dstates, lam, dq, dk, total; int hpc; };
+struct Workspace { size_t ckpt, dstates, lam, dq, dk, total; GradPlan grad; };
 Workspace bwd_layout(const m2rnn_delta_params *p, bool have_ckpt) {
   Workspace w{};
   const size_t tokens = tokens_of(p), slots = delta_slots(p, tokens, chunk_of(p)), units = slots * p->N;
   size_t off = have_ckpt ? 0 : ckpt_layout(p).total;
   const bool f32 = p->io_dtype == M2RNN_F32;
-  w.hpc = f32 ? 1 : delta_grad_heads(p, slots);
+  w.grad = f32 ? GradPlan{1, 0} : delta_grad_plan(p, slots);
+  const int hpc = w.grad.heads;
   w.dstates = off;
   off += align_up(units * p->K * p->V * (f32 ? 4 : 2));
   w.lam = off;
   off += align_up(units * chunk_of(p) * p->V * (f32 ? 4 : 2));
-  const size_t shares = tokens * (p->N / w.hpc) * p->K * sizeof(float);
+  const size_t shares = tokens * (p->N / hpc) * p->K * sizeof(float);
   w.dq = off;
-  if (p->N / p->Nq > w.hpc) off += align_up(shares);
+  if (p->N / p->Nq > hpc) off += align_up(shares);
   w.dk = off;
-  if (p->N / p->Nk > w.hpc) off += align_up(shares);
+  if (p->N / p->Nk > hpc) off += align_up(shares);
   w.total = off;
   return w;
 }
@@ -179,10 +180,10 @@ int m2rnn_delta_bwd(const m2rnn_delta_params *params, const void *q, const void 
     if (e != cudaSuccess) return cuda_failed();
   }
   a.dy = dy; a.d_hT = d_hT; a.dq = dq; a.dk = dk; a.dv = dv; a.dgate = dgate; a.dstep = dstep; a.dh0 = dh0;
-  a.hpc = w.hpc;
-  a.shares = params->N / w.hpc;
-  a.dq_part = params->N / params->Nq > w.hpc ? reinterpret_cast<float *>(ws + w.dq) : nullptr;
-  a.dk_part = params->N / params->Nk > w.hpc ? reinterpret_cast<float *>(ws + w.dk) : nullptr;
+  a.hpc = w.grad.heads; a.grad_ctas = w.grad.ctas;
+  a.shares = params->N / a.hpc;
+  a.dq_part = params->N / params->Nq > a.hpc ? reinterpret_cast<float *>(ws + w.dq) : nullptr;
+  a.dk_part = params->N / params->Nk > a.hpc ? reinterpret_cast<float *>(ws + w.dk) : nullptr;
   cudaError_t e;
   const Ckpt c = ckpt_layout(params);
   a.rec = kept + c.rec; a.states = kept + c.states; a.upd = kept + c.upd;

@@ -18,6 +18,9 @@
 // chains have, so half the chains to an SM.)  What is kept for the gradient goes from registers to memory, 128 bytes an instruction.
 // Roundings to bf16: the operands S, X, U (dS, dU, L), the factored e^(g_last - g) U and the like, and T and P.  S itself
 // is held and updated in fp32.
+// Bound by the chain's latency where an SM has a chain to a scheduler (1 001 tokens, 84 heads of 64 x 16: 19.0 us, 0.55 a chunk), by shared
+// memory's bandwidth where it has more (LSU data pipe 86 % busy; 8 x 2 048 tokens, 16 heads of 64 x 64: 49.5 us; 65 536 tokens, 32 heads of
+// 128 x 128: 1 576 us, 0.77 a chunk of two chains).
 #include <algorithm>
 
 #include "delta_common.cuh"
@@ -618,7 +621,7 @@ __global__ void __launch_bounds__(160, 2) delta_chain_bwd_kernel(DeltaArgs a, in
 
 // 16-column warps of a CTA: four (they share the copies of k, q and the records), two or one where that leaves a quarter fewer chains to
 // the SM that has the most: chains of an SM share its shared memory's bandwidth (65 536 tokens, 32 heads of 128 x 128: 64 CTAs of four
-// 2 403 us, 128 of two 1 609).
+// 2 354 us, 128 of two 1 576).
 ChainPlan plan_chain(const DeltaArgs &a) {
   const int cols = a.V / 16;
   const long long units = (long long)a.B * a.N, sms = sm_count();

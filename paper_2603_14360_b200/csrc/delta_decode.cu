@@ -7,11 +7,12 @@
 // a warp takes 32 / L rows at a time; sixteen 16-byte loads of a lane are in flight at once (fewer where the state is
 // smaller).  W warps share a unit: the sums over rows go through shuffles, then (W > 1) through shared memory.  Everything
 // is fp32, whatever the types in memory.
+// 512 rows of 32 bf16 states of 128 x 128: 198 us, 5.4 TB/s; 48 rows of 84 fp32 states of 64 x 16: 7.1 us (4.7 TB/s with the launch);
+// one row of these: 3.9 us, a launch and a memory round trip.
 #include "delta_common.cuh"
 
 namespace m2rnn {
 namespace {
-
 
 // 16 bytes of a state, as they lie in memory, and as floats
 template <typename TS> struct Vec16;

@@ -15,24 +15,28 @@
 // (With q . dq - k . dk in place of R, W and G the pairs on one side of t would cancel only up to the roundings of
 // the matrices to bf16: 2.5e-2 off where states decay within a few tokens.  Here the same fp32 value is added and taken away.)
 //
-// 2 KG warps: 16 tokens x one of KG parts of the K features each; the products over V in slabs of 64 columns (32 where K > 64).
+// 2 KG warps: 16 tokens x one of KG parts of the K features each; the products over V in slabs of 64 columns (32 where K > 64 or where
+// heads share q and k).  (Four parts: half the accumulators a thread, but every warp loads all of dY, L and U; slower at three CTAs to an SM.)
 // A job is a chunk of `hpc` heads that share q and k, one after the other: their X1, X2, dq', dk' are added up in registers, and the products
-// with Q and K, which are the same for all of them, taken once.  Two CTAs
-// to an SM walk over the jobs, the next slab (and the next job's rows) on its way while one is worked on: with a CTA a job the
-// loads' latency stood between a third of the cycles.  What the chains wrote is contiguous and comes by untiled bulk
-// copies; rows of q, k, v and dY by cp.async.
+// with Q and K, which are the same for all of them, taken once.  Two or three CTAs to an SM (delta_grad_plan) walk over the jobs, the next slab
+// (and the next job's rows) on its way while one is worked on: with a CTA a job the loads' latency stood between a third of the cycles.  Where
+// both buffers of a slab leave no room for a third CTA (V = 64, heads of their own) there is one buffer: 469 us for the second shape below, 497
+// with two and two.  What the chains wrote is contiguous and comes by untiled bulk copies; rows of q, k, v and dY by cp.async; results go straight to
+// memory, 16 bytes of a row an instruction.
+// 16 384 tokens, 84 heads of 64 x 16 on one q and k: 351 us; 32 768 tokens, 32 heads of 64 x 64: 469 us, 49 KB a chunk and head or 3.4 TB/s;
+// 25 026 packed tokens, 16 heads of 128 x 128: 425 us.  Bound by the latency of its products, shuffles and shared-memory reads.
 #include "delta_common.cuh"
 
 namespace m2rnn {
 namespace {
 
-constexpr int C = kDeltaChunk;
+constexpr int C = kDeltaChunk, KG = 2;
 
-template <int K, int KG> struct GradCfg {
+template <int K> struct GradCfg {
   static constexpr int kThreads = 64 * KG;
   static constexpr int kPK = 2 * K + 16;
   static constexpr int kRows = 2 * C * kPK, kMat = 2 * kRows;            // q, k rows, twice; X1, X2 as blocks
-  static constexpr int kRed = kMat + 2 * 2048;                           // sums, see Red
+  static constexpr int kRed = kMat + 2 * 2048;                           // sums: rows as named below
   static constexpr int kSlab = kRed + (5 * KG + 7) * 128;                // slabs: the vectors, dY, V rows, then U, L, S, dS' blocks
   static constexpr int NT = (K / 8 + KG - 1) / KG;                       // 8-feature tiles of a warp, most
   static constexpr int JT = 4 / KG;                                      // 8-token tiles of a warp's part of a 16 x 32 product
@@ -46,9 +50,9 @@ __host__ __device__ constexpr int slab_bytes(int K, int VS) { return 1024 + 2 * 
 struct GradJob { long long tok; size_t slot; int have, n0, run, hq, hk; };      // have = 0: no more
 
 // MULTI: several heads to a job; VS: columns of a slab
-template <int K, int KG, bool MULTI, int VS, int BUFS, int CTAS>
+template <int K, bool MULTI, int VS, int BUFS, int CTAS>
 __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, unsigned jobs) {
-  using Cfg = GradCfg<K, KG>;
+  using Cfg = GradCfg<K>;
   constexpr int NT = Cfg::NT, JT = Cfg::JT, kThreads = Cfg::kThreads, kIdle = 2 * (KG - 1);
   constexpr int pv = 2 * VS + 16, P = VS / 8, slab = slab_bytes(K, VS), UB = 2 * C * VS, SB = 2 * K * VS;      // P: pieces of a row; bytes of U, of S
   extern __shared__ __align__(128) unsigned char smem[];
@@ -447,17 +451,21 @@ __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, 
   }
 }
 
-template <int K, bool MULTI, int VS> cudaError_t launch_kmv(const DeltaArgs &a, cudaStream_t s) {
-  constexpr int KG = 2, CTAS = K > 64 ? 2 : 3;
-  using Cfg = GradCfg<K, KG>;
+template <int K, bool MULTI, int VS, int CTAS> cudaError_t launch_kmvc(const DeltaArgs &a, cudaStream_t s) {
+  using Cfg = GradCfg<K>;
   constexpr int room = 227 * 1024 / CTAS - 1024, BUFS = MULTI || Cfg::kSlab + 2 * slab_bytes(K, VS) <= room ? 2 : 1;
   constexpr size_t smem = Cfg::kSlab + BUFS * (size_t)slab_bytes(K, VS);
   static_assert(smem <= room, "CTAs to an SM");
-  const auto kernel = delta_grad_kernel<K, KG, MULTI, VS, BUFS, CTAS>;
+  const auto kernel = delta_grad_kernel<K, MULTI, VS, BUFS, CTAS>;
   const cudaError_t e = allow_smem(kernel, smem);
   if (e != cudaSuccess) return e;
   const unsigned jobs = (unsigned)(a.slots * (a.N / a.hpc)), most = CTAS * (unsigned)sm_count();
   return launch_early(kernel, dim3(jobs < most ? jobs : most), dim3(Cfg::kThreads), smem, s, a, jobs);
+}
+template <int K, bool MULTI, int VS> cudaError_t launch_kmv(const DeltaArgs &a, cudaStream_t s) {
+  if constexpr (K > 64) return launch_kmvc<K, MULTI, VS, 2>(a, s);
+  else if constexpr (!MULTI) return launch_kmvc<K, MULTI, VS, 3>(a, s);
+  else return a.grad_ctas == 2 ? launch_kmvc<K, MULTI, VS, 2>(a, s) : launch_kmvc<K, MULTI, VS, 3>(a, s);
 }
 template <int K, bool MULTI> cudaError_t launch_km(const DeltaArgs &a, cudaStream_t s) {
   constexpr int VS = MULTI || K > 64 ? 32 : 64;
@@ -469,17 +477,20 @@ template <int K> cudaError_t launch_k(const DeltaArgs &a, cudaStream_t s) { retu
 
 }  // namespace
 
-// Heads of a job, of those that share q and k: the most that keep the CTAs (two to an SM) busy for as few heads one after
-// the other as there can be
-int delta_grad_heads(const m2rnn_delta_params *p, size_t slots) {
-  int run = p->N / p->Nq, o = p->N / p->Nk, best = 1;
+// Heads of a job, of those that share q and k, and CTAs to an SM: what leaves an SM the least to do, a job counted as its heads and half a
+// head for what it does once.  Above K = 64 registers and shared memory have room for two CTAs; up to there three fill an SM, but of several
+// heads two do 6 % more (16 384 tokens, 84 heads of 64 x 16: 351 us against 371), unless the jobs come out as one round of three.
+GradPlan delta_grad_plan(const m2rnn_delta_params *p, size_t slots) {
+  int run = p->N / p->Nq, o = p->N / p->Nk;
   while (o) { const int t = run % o; run = o; o = t; }
+  GradPlan best{1, 2};
   size_t least = ~(size_t)0;
-  for (int d = run; d >= 1; --d) {
-    if (run % d) continue;
-    const size_t ctas = (size_t)(p->K > 64 ? 2 : 3) * sm_count(), rounds = (slots * (p->N / d) + ctas - 1) / ctas * d;
-    if (rounds + rounds / 32 < least) { least = rounds; best = d; }      // (fewer heads only where that saves 3 %: more shares to add up)
-  }
+  for (int d = run; d >= 1; --d)
+    for (int ctas = 2; ctas <= 3; ++ctas) {
+      if (run % d || (p->K > 64 ? ctas == 3 : d == 1 && ctas == 2)) continue;
+      const size_t round = (size_t)ctas * sm_count(), cost = (slots * (p->N / d) + round - 1) / round * ctas * (2 * d + 1) * (d > 1 && ctas == 3 ? 17 : 16);
+      if (cost + cost / 32 < least) { least = cost; best = GradPlan{d, ctas}; }      // (fewer heads only where that saves 3 %: more shares to add up)
+    }
   return best;
 }
 

@@ -141,6 +141,14 @@ def test_many_shared_heads(dtype):
     assert max(errs.values()) <= TOL[dtype], errs
 
 
+@pytest.mark.parametrize("K,V", [(16, 16), (48, 128), (64, 32), (64, 16)])
+@pytest.mark.parametrize("B,N", [(100, 8), (9, 6), (150, 4)])
+def test_jobs_of_the_gradient_kernel(B, N, K, V):
+    """Numbers of chunks and heads for which it takes two and three CTAs to an SM, and one head and several to a job."""
+    errs = run_both(seed=16, B=B, T=5, N=N, K=K, V=V, Nq=1, Nk=1)
+    assert max(errs.values()) <= TOL[BF], errs
+
+
 def test_keys_that_point_the_same_way():
     """T's diagonal blocks by substitution: with equal keys and steps of 1 M is a triangle of ones."""
     x, on, H0, dy, d_hT, o = make(8, B=1, T=96, N=2, K=64, V=32, gate="log", step="value")
