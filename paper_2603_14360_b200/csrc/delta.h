@@ -104,7 +104,7 @@ cudaError_t launch_delta_fwd_f32(const DeltaArgs &a, cudaStream_t s);     // del
 cudaError_t launch_delta_bwd_f32(const DeltaArgs &a, cudaStream_t s);
 
 struct DeltaStepArgs {
-  int B, N, Nq, Nk, K, V;
+  int B, N, Nq, Nk, K, V, per_q, per_k;      // per: as in DeltaArgs
   int gate_kind, step_kind, qk_norm;
   float eps, scale;
   const void *q, *k, *v, *gate, *step;

@@ -214,6 +214,7 @@ int m2rnn_delta_decode_step(const m2rnn_delta_params *params, const void *q, con
     if (!aligned16(p)) return M2RNN_ERR_ALIGN;
   DeltaStepArgs a{};
   a.B = params->B; a.N = params->N; a.Nq = params->Nq; a.Nk = params->Nk; a.K = params->K; a.V = params->V;
+  a.per_q = params->N / params->Nq; a.per_k = params->N / params->Nk;
   a.gate_kind = params->gate_kind; a.step_kind = params->step_kind; a.qk_norm = params->qk_norm != 0; a.eps = params->norm_eps; a.scale = params->q_scale;
   a.q = q; a.k = k; a.v = v; a.gate = gate; a.step = step; a.alpha = alpha; a.beta = beta;
   a.state = state; a.y = y; a.slots = slots; a.nslots = n_slots; a.dev_status = dev_status;

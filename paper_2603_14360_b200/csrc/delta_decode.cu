@@ -7,8 +7,11 @@
 // a warp takes 32 / L rows at a time; sixteen 16-byte loads of a lane are in flight at once (fewer where the state is
 // smaller).  W warps share a unit: the sums over rows go through shuffles, then (W > 1) through shared memory.  Everything
 // is fp32, whatever the types in memory.
-// 512 rows of 32 bf16 states of 128 x 128: 198 us, 5.4 TB/s; 48 rows of 84 fp32 states of 64 x 16: 7.1 us (4.7 TB/s with the launch);
-// one row of these: 3.9 us, a launch and a memory round trip.
+// What is the same for a unit (lengths, decay, step) its first warp works out for the others, a warp loads the rows of k and q that it has rows of
+// the state for, and v is asked for before anything is waited for: with every warp working all of it out, and loops of a length not known to
+// the compiler, the kernel was bound by its instructions (81 % of the issue slots, 1 440 a warp: 198, 7.1 and 3.9 us below).
+// 512 rows of 32 bf16 states of 128 x 128: 178 us, 6.0 TB/s; 48 rows of 84 fp32 states of 64 x 16: 6.0 us; one row of these: 3.0 us, a launch
+// and a memory round trip.
 #include "delta_common.cuh"
 
 namespace m2rnn {
@@ -33,78 +36,122 @@ template <> struct Vec16<__nv_bfloat16> {
   __device__ static uint4 close(const float (&x)[8]) { return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])); }
 };
 
-// R: 16-byte pieces of a lane, most; W warps to a unit, kWarps to a CTA
-template <typename TIO, typename TS, int V, int R, int kWarps>
-__global__ void __launch_bounds__(32 * kWarps, (R > 8 ? 16 : sizeof(TS) == 2 ? 32 : 28) / kWarps) delta_step_kernel(DeltaStepArgs a, int W) {
+// k and q of a row, side by side in shared memory; the sums of both products over a piece's columns
+template <typename TIO, typename TS> struct Pair {
+  float k, q;
+  __device__ Pair(TIO k, TIO q) : k(to_f32(k)), q(to_f32(q)) {}
+  __device__ float key() const { return k; }
+  template <int E> __device__ void add(const uint4 &r, float (&sk)[E], float (&sq)[E]) const {
+    float h[E];
+    Vec16<TS>::open(r, h);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      sk[e] = fmaf(h[e], k, sk[e]);
+      sq[e] = fmaf(h[e], q, sq[e]);
+    }
+  }
+};
+template <> struct Pair<__nv_bfloat16, __nv_bfloat16> {      // (as they are: products of 16-bit operands in fp32, nothing to unpack)
+  uint32_t kq;
+  __device__ Pair(__nv_bfloat16 k, __nv_bfloat16 q) : kq((uint32_t)__bfloat16_as_ushort(q) << 16 | __bfloat16_as_ushort(k)) {}
+  __device__ float key() const { return __uint_as_float(kq << 16); }
+  __device__ void add(const uint4 &r, float (&sk)[8], float (&sq)[8]) const {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sk[2 * i] = fma_bf16<0, 0>(w[i], kq, sk[2 * i]);
+      sk[2 * i + 1] = fma_bf16<1, 0>(w[i], kq, sk[2 * i + 1]);
+      sq[2 * i] = fma_bf16<0, 1>(w[i], kq, sq[2 * i]);
+      sq[2 * i + 1] = fma_bf16<1, 1>(w[i], kq, sq[2 * i + 1]);
+    }
+  }
+};
+
+// R: 16-byte pieces of a lane (FULL: as many, else at most); 2^log_w warps to a unit, kWarps to a CTA
+template <typename TIO, typename TS, int V, int R, int kWarps, bool FULL>
+__global__ void __launch_bounds__(32 * kWarps, (R > 8 ? 16 : sizeof(TS) == 2 ? 32 : 28) / kWarps) delta_step_kernel(DeltaStepArgs a, int log_w) {
   using X = Vec16<TS>;
-  constexpr int E = X::n, L = V / E, G = 32 / L;     // lanes to a row, rows of a warp at a time
-  __shared__ float part[kWarps][2][V];               // sums over a warp's rows; then [unit's first warp][0]: u
-  __shared__ float ksm[kWarps][128], qsm[kWarps][128];
+  using KQ = Pair<TIO, TS>;
+  constexpr int E = X::n, L = V / E, G = 32 / L, NX = (V + 31) / 32;     // lanes to a row, rows of a warp at a time; columns of u a lane, most
+  __shared__ float part[kWarps][2][V];               // sums over a warp's rows; then [unit's first warp][0]: u / |k|
+  __shared__ float scalars[kWarps][6];               // of a unit, at its first warp
+  __shared__ alignas(8) unsigned char kq_of[kWarps][128 * sizeof(KQ)];      // a warp's rows
   begin_dependent();
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, col = (lane % L) * E;
-  const int unit0 = warp / W, sub = warp % W;        // the CTA's unit, this warp's share of it
-  const long long unit = (long long)blockIdx.x * (kWarps / W) + unit0;
+  const int W = 1 << log_w, first = warp & -W, sub = warp & (W - 1);      // the unit's first warp, this one's share of it
+  const unsigned unit = blockIdx.x * (unsigned)(kWarps >> log_w) + (unsigned)(warp >> log_w);
   const int K = a.K, N = a.N;
-  const bool in = unit < (long long)a.B * N;
-  const int b = in ? (int)(unit / N) : 0, n = in ? (int)(unit % N) : 0;
-  const size_t bn = (size_t)b * N + n;
-  int slot = b;
-  if (a.slots && in) slot = a.slots[b];
-  // what does not hang on the slot is asked for first
-  const TIO *kg = static_cast<const TIO *>(a.k) + ((size_t)b * a.Nk + n / (N / a.Nk)) * K, *qg = static_cast<const TIO *>(a.q) + ((size_t)b * a.Nq + n / (N / a.Nq)) * K;
-  float kx[4] = {}, qx[4] = {};
+  const bool in = unit < (unsigned)a.B * (unsigned)N;
+  const unsigned bn = in ? unit : 0u, b = bn / (unsigned)N, n = bn - b * (unsigned)N;
+  const int slot = a.slots ? a.slots[b] : (int)b;
+  // what does not hang on the slot is asked for first: this warp's rows of k and q (the first one's: all, for their lengths), gates, v
+  const int rows = K >> log_w, row0 = sub * rows, count = !in ? 0 : sub ? rows : K;
+  const TIO *kg = static_cast<const TIO *>(a.k) + ((size_t)b * a.Nk + n / (unsigned)a.per_k) * K + row0 + lane;
+  const TIO *qg = static_cast<const TIO *>(a.q) + ((size_t)b * a.Nq + n / (unsigned)a.per_q) * K + row0 + lane;
+  TIO kx[4], qx[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (in && lane + 32 * i < K) { kx[i] = to_f32(kg[lane + 32 * i]); qx[i] = to_f32(qg[lane + 32 * i]); }
-  const float gate = in ? to_f32(static_cast<const TIO *>(a.gate)[bn]) : 0.f, step_in = in ? to_f32(static_cast<const TIO *>(a.step)[bn]) : 0.f;
-  const bool psi = a.gate_kind == M2RNN_GATE_PSI;
-  const float alpha = psi && in ? a.alpha[n] : 1.f, beta = psi && in ? a.beta[n] : 0.f;
+  for (int i = 0; i < 4; ++i) {
+    kx[i] = qx[i] = from_f32<TIO>(0.f);
+    if (lane + 32 * i < count) { kx[i] = kg[32 * i]; qx[i] = qg[32 * i]; }
+  }
+  float gate = 0.f, step_in = 0.f, alpha = 1.f, beta = 0.f;
+  if (in && sub == 0) {
+    gate = to_f32(static_cast<const TIO *>(a.gate)[bn]);
+    step_in = to_f32(static_cast<const TIO *>(a.step)[bn]);
+    if (a.gate_kind == M2RNN_GATE_PSI) { alpha = a.alpha[n]; beta = a.beta[n]; }
+  }
+  float vx[NX];
+#pragma unroll
+  for (int i = 0; i < NX; ++i) {
+    const int x = 32 * (sub + (i << log_w)) + lane;
+    vx[i] = in && x < V ? to_f32(static_cast<const TIO *>(a.v)[(size_t)bn * V + x]) : 0.f;
+  }
   // a negative slot is a padding row: no state, y = 0.  One outside the pool is reported.
   const bool live = in && slot >= 0 && slot < a.nslots;
   if (in && slot >= a.nslots && a.dev_status && lane == 0) atomicExch(a.dev_status, (int32_t)M2RNN_ERR_SHAPE);
-  const int per = K / (G * W), row0 = sub * per * G + lane / L;      // this lane's rows: row0 + r G
-  TS *st = static_cast<TS *>(a.state) + ((size_t)(live ? slot : 0) * N + n) * K * V + (size_t)row0 * V + col;
+  const int per = rows / G, mine = lane / L;      // pieces of a lane, its place in a group of rows
+  TS *st = static_cast<TS *>(a.state) + ((size_t)(live ? slot : 0) * N + n) * K * V + (size_t)(row0 + mine) * V + col;
   uint4 H[R];
   if (live) {
 #pragma unroll
     for (int r = 0; r < R; ++r)
-      if (r < per) H[r] = __ldcs(reinterpret_cast<const uint4 *>(st + (size_t)(r * G) * V));
+      if (FULL || r < per) H[r] = __ldcs(reinterpret_cast<const uint4 *>(st + r * G * V));
   }
-  // q and k of the unit: every warp keeps its own copy in shared memory
-  float kk = 0.f, qq = 0.f, qk = 0.f;
+  KQ *kq = reinterpret_cast<KQ *>(kq_of[warp]);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (lane + 32 * i < K) { ksm[warp][lane + 32 * i] = kx[i]; qsm[warp][lane + 32 * i] = qx[i]; }
-    kk = fmaf(kx[i], kx[i], kk);
-    qq = fmaf(qx[i], qx[i], qq);
-    qk = fmaf(qx[i], kx[i], qk);
-  }
+  for (int i = 0; i < 4; ++i)
+    if (lane + 32 * i < rows) kq[lane + 32 * i] = KQ(kx[i], qx[i]);
+  if (sub == 0) {      // lengths, decay and step
+    float kk = 0.f, qq = 0.f, qk = 0.f;
 #pragma unroll
-  for (int d = 16; d; d /= 2) {
-    kk += __shfl_xor_sync(0xffffffffu, kk, d);
-    qq += __shfl_xor_sync(0xffffffffu, qq, d);
-    qk += __shfl_xor_sync(0xffffffffu, qk, d);
+    for (int i = 0; i < 4; ++i) {
+      const float k = to_f32(kx[i]), q = to_f32(qx[i]);
+      kk = fmaf(k, k, kk);
+      qq = fmaf(q, q, qq);
+      qk = fmaf(q, k, qk);
+    }
+#pragma unroll
+    for (int d = 16; d; d /= 2) {
+      kk += __shfl_xor_sync(0xffffffffu, kk, d);
+      qq += __shfl_xor_sync(0xffffffffu, qq, d);
+      qk += __shfl_xor_sync(0xffffffffu, qk, d);
+    }
+    const float rk = a.qk_norm ? 1.f / sqrtf(kk + a.eps) : 1.f, rq = a.scale * (a.qk_norm ? 1.f / sqrtf(qq + a.eps) : 1.f);
+    float unused;
+    const float decay = expf(delta_log_decay(a.gate_kind, gate, alpha, beta, unused)), step = delta_step_of(a.step_kind, step_in, unused);
+    if (lane == 0) {
+      float *f = scalars[warp];
+      f[0] = decay; f[1] = step; f[2] = -decay * rk; f[3] = rq * decay; f[4] = rq * (rk * qk); f[5] = rk;
+    }
   }
   __syncwarp();
-  const float rk = a.qk_norm ? 1.f / sqrtf(kk + a.eps) : 1.f, rq = a.scale * (a.qk_norm ? 1.f / sqrtf(qq + a.eps) : 1.f);
-  float unused;
-  const float decay = expf(delta_log_decay(a.gate_kind, gate, alpha, beta, unused)), step = delta_step_of(a.step_kind, step_in, unused);
   float sk[E], sq[E];      // H^T k, H^T q
 #pragma unroll
   for (int e = 0; e < E; ++e) sk[e] = sq[e] = 0.f;
   if (live) {
 #pragma unroll
     for (int r = 0; r < R; ++r)
-      if (r < per) {
-        const float k = ksm[warp][row0 + r * G], q = qsm[warp][row0 + r * G];
-        float h[E];
-        X::open(H[r], h);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          sk[e] = fmaf(h[e], k, sk[e]);
-          sq[e] = fmaf(h[e], q, sq[e]);
-        }
-      }
+      if (FULL || r < per) kq[mine + r * G].add(H[r], sk, sq);
   }
 #pragma unroll
   for (int d = L; d < 32; d *= 2)
@@ -123,50 +170,57 @@ __global__ void __launch_bounds__(32 * kWarps, (R > 8 ? 16 : sizeof(TS) == 2 ? 3
   }
   if (W > 1) __syncthreads();
   else __syncwarp();
-  for (int x = sub * 32 + lane; x < V; x += 32 * W) {
+  const float *f = scalars[first];
+#pragma unroll
+  for (int i = 0; i < NX; ++i) {
+    const int x = 32 * (sub + (i << log_w)) + lane;
+    if (x >= V) break;
     float s = 0.f, t = 0.f;
-    for (int w = unit0 * W; w < unit0 * W + W; ++w) { s += part[w][0][x]; t += part[w][1][x]; }
-    const float u = in ? step * fmaf(-decay * rk, s, to_f32(static_cast<const TIO *>(a.v)[bn * V + x])) : 0.f;
-    part[unit0 * W][0][x] = u;      // (its place is read, by this lane)
-    if (in) static_cast<TIO *>(a.y)[bn * V + x] = from_f32<TIO>(live ? rq * fmaf(decay, t, rk * qk * u) : 0.f);
+    for (int w = first; w < first + W; ++w) { s += part[w][0][x]; t += part[w][1][x]; }
+    const float u = f[1] * fmaf(f[2], s, vx[i]);
+    part[first][0][x] = f[5] * u;      // (its place is read, by this lane)
+    if (in) static_cast<TIO *>(a.y)[(size_t)bn * V + x] = from_f32<TIO>(live ? fmaf(f[3], t, f[4] * u) : 0.f);
   }
   if (W > 1) __syncthreads();
   else __syncwarp();
   if (!live) return;
+  const float decay = f[0];
   float u[E];
 #pragma unroll
   for (int e = 0; e < E; e += 4) {
-    const float4 f = *reinterpret_cast<const float4 *>(&part[unit0 * W][0][col + e]);
-    u[e] = f.x; u[e + 1] = f.y; u[e + 2] = f.z; u[e + 3] = f.w;
+    const float4 p = *reinterpret_cast<const float4 *>(&part[first][0][col + e]);
+    u[e] = p.x; u[e + 1] = p.y; u[e + 2] = p.z; u[e + 3] = p.w;
   }
 #pragma unroll
   for (int r = 0; r < R; ++r)
-    if (r < per) {
-      const float k = rk * ksm[warp][row0 + r * G];
+    if (FULL || r < per) {
+      const float k = kq[mine + r * G].key();
       float h[E];
       X::open(H[r], h);
 #pragma unroll
       for (int e = 0; e < E; ++e) h[e] = fmaf(k, u[e], decay * h[e]);
-      __stcs(reinterpret_cast<uint4 *>(st + (size_t)(r * G) * V), X::close(h));
+      __stcs(reinterpret_cast<uint4 *>(st + r * G * V), X::close(h));
     }
 }
 
+template <typename TIO, typename TS, int V, int R, int kWarps> cudaError_t launch_r(const DeltaStepArgs &a, int log_w, int per, cudaStream_t s) {
+  const dim3 g((unsigned)((((long long)a.B * a.N << log_w) + kWarps - 1) / kWarps)), t(32 * kWarps);
+  return per == R ? launch_early(delta_step_kernel<TIO, TS, V, R, kWarps, true>, g, t, 0, s, a, log_w) : launch_early(delta_step_kernel<TIO, TS, V, R, kWarps, false>, g, t, 0, s, a, log_w);
+}
 template <typename TIO, typename TS, int V> cudaError_t launch_v(const DeltaStepArgs &a, cudaStream_t s) {
   constexpr int E = Vec16<TS>::n, G = 32 / (V / E), R = sizeof(TS) == 4 ? 16 : 8;      // 64 entries of a state a lane, most
   // warps to a unit: a power of two that leaves whole groups of rows and at most R pieces a lane
-  constexpr int most = 8;
-  int W = 1;
-  while (W < most && a.K / (G * W) > R) W *= 2;
+  constexpr int most = 3;
+  int log_w = 0;
+  while (log_w < most && a.K >> log_w > G * R) ++log_w;
   const long long units = (long long)a.B * a.N;
   // few units: more warps to each, while every one has a group of rows
-  while (W < most && a.K % (2 * W * G) == 0 && units * W * 2 <= (long long)sm_count() * 8) W *= 2;
+  while (log_w < most && a.K % (G << (log_w + 1)) == 0 && units << (log_w + 1) <= (long long)sm_count() * 8) ++log_w;
   // CTAs of four warps fill an SM's registers closer than those of eight (28 warps against 24: the units of 48 sequences of 84 heads at
   // once instead of in two rounds)
-  const int warps = W > 4 ? 8 : 4;
-  const dim3 g((unsigned)((units * W + warps - 1) / warps)), t(32 * warps);
-  const bool half = a.K / (G * W) <= R / 2;
-  if (warps == 8) return half ? launch_early(delta_step_kernel<TIO, TS, V, R / 2, 8>, g, t, 0, s, a, W) : launch_early(delta_step_kernel<TIO, TS, V, R, 8>, g, t, 0, s, a, W);
-  return half ? launch_early(delta_step_kernel<TIO, TS, V, R / 2, 4>, g, t, 0, s, a, W) : launch_early(delta_step_kernel<TIO, TS, V, R, 4>, g, t, 0, s, a, W);
+  const int per = (a.K >> log_w) / G;
+  if (log_w > 2) return per <= R / 2 ? launch_r<TIO, TS, V, R / 2, 8>(a, log_w, per, s) : launch_r<TIO, TS, V, R, 8>(a, log_w, per, s);
+  return per <= R / 2 ? launch_r<TIO, TS, V, R / 2, 4>(a, log_w, per, s) : launch_r<TIO, TS, V, R, 4>(a, log_w, per, s);
 }
 template <typename TIO, typename TS> cudaError_t launch_t(const DeltaStepArgs &a, cudaStream_t s) {
   switch (a.V) {
