@@ -19,7 +19,7 @@
 // Roundings to bf16: the operands S, X, U (dS, dU, L), the factored e^(g_last - g) U and the like, and T and P.  S itself
 // is held and updated in fp32.
 // Bound by the chain's latency where an SM has a chain to a scheduler (1 001 tokens, 84 heads of 64 x 16: 19.0 us, 0.55 a chunk), by shared
-// memory's bandwidth where it has more (LSU data pipe 86 % busy; 8 x 2 048 tokens, 16 heads of 64 x 64: 49.5 us; 65 536 tokens, 32 heads of
+// memory's bandwidth where it has more (LSU data pipe 83 % busy with two; 8 x 2 048 tokens, 16 heads of 64 x 64: 49.5 us; 65 536 tokens, 32 heads of
 // 128 x 128: 1 576 us, 0.77 a chunk of two chains).
 #include <algorithm>
 
