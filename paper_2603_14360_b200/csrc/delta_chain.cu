@@ -14,13 +14,14 @@
 // A chunk's chain is S -> X -> U -> S', each step a product whose last results the next one waits for.  What is not on it fills the
 // waits, in one stretch of code without branches that the compiler orders: forward the products of the chunk before's Y (S of that
 // chunk as operands from shared memory, tile by tile before the new ones take their places), backward those with Q.
-// (Y after its own chunk's chain: 1 680 cycles a chunk of K = 64 for a warp alone; Y in warps of their own: as many registers as the
-// chains have, so half the chains to an SM.)  What is kept for the gradient goes from registers to memory, 128 bytes an instruction.
+// (Y after its own chunk's chain: 1 680 cycles a chunk of K = 64 for a warp alone.)  Where SMs have warps to spare, Y is a warp's of its own beside
+// each chain: it finds the chunk's S and U in one of two buffers that the chain fills.  (plan_chain; where they have not, those warps would halve
+// the chains to an SM.)  What is kept for the gradient goes from registers to memory, 128 bytes an instruction.
 // Roundings to bf16: the operands S, X, U (dS, dU, L), the factored e^(g_last - g) U and the like, and T and P.  S itself
 // is held and updated in fp32.
-// Bound by the chain's latency where an SM has a chain to a scheduler (1 001 tokens, 84 heads of 64 x 16: 19.0 us, 0.55 a chunk), by shared
-// memory's bandwidth where it has more (LSU data pipe 83 % busy with two; 8 x 2 048 tokens, 16 heads of 64 x 64: 49.5 us; 65 536 tokens, 32 heads of
-// 128 x 128: 1 576 us, 0.77 a chunk of two chains).
+// Bound by the chain's latency where an SM has a chain to a scheduler (1 001 tokens, 84 heads of 64 x 16: 15.9 us, 0.45 a chunk; 65 536 tokens,
+// 32 heads of 128 x 128, two chains to an SM: 1 383 us, 0.68 a chunk; 8 x 2 048 tokens, 16 heads of 64 x 64, four: 49.5 us, 0.77), by shared memory's
+// bandwidth where it has more (two to a scheduler: LSU data pipe 83 % busy).
 #include <algorithm>
 
 #include "delta_common.cuh"
@@ -39,7 +40,10 @@ __host__ __device__ constexpr int stage_bytes(int K, int nw) { return C * (2 * p
 // [column tile][feature tile].  (Shared memory's bandwidth is what chains of an SM compete for: 324 of its cycles a chain and chunk of K = 64.)
 __host__ __device__ constexpr int out_bytes(int K) { return K <= 64 ? 0 : 32 * K; }
 
-struct ChainPlan { int nw, slabs, stages; size_t smem; };      // nw: 16-column warps of a CTA
+// S and U of a chunk for a warp that does Y
+__host__ __device__ constexpr int apart_bytes(int K) { return 32 * K + 1024; }
+
+struct ChainPlan { int nw, slabs, stages, apart; size_t smem; };      // nw: 16-column warps of a CTA
 
 // What a CTA has to do: batch entry, head, and which slab of its columns
 struct ChainWork { int b, n, slab; };
@@ -303,26 +307,28 @@ __device__ __forceinline__ void rows_out(const float (&x)[4][4], uint32_t at, ui
   }
 }
 
-// Barriers of a CTA: stages filled and free
-struct ChainBars { uint64_t full[8], empty[8]; };
+// Barriers of a CTA: stages filled and free; a chain's S and U there for its Y's warp, and taken
+struct ChainBars { uint64_t full[8], empty[8], ready[8], taken[8]; };      // (ready, taken: two buffers of a chain)
 
-// A warp's part: 0 .. nw - 1 a chain, nw copies, above that none.  An SM's CTAs come a layer after the other, and warp w of the SM's
+// A warp's part: 0 .. nw - 1 a chain, nw copies, above that none; apart: nw .. 2 nw - 1 the chains' Y, 2 nw copies.  An SM's CTAs come a layer after the other, and warp w of the SM's
 // belongs to scheduler w % 4: with CTAs of two warps (a chain) or four (two) the parts of every second pair of layers, or layer, change
 // places, so that chains share a scheduler only where there are more than four to the SM.
-__device__ __forceinline__ int chain_role(const DeltaArgs &a, int nw) {
+__device__ __forceinline__ int chain_role(const DeltaArgs &a, int nw, bool apart) {
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), layer = (int)(blockIdx.x / (unsigned)a.sms);
+  if (apart) return nw == 2 && warp >= 4 ? (warp == 6 ? 4 : 5) : warp;
   if (nw == 1) return warp ^ (layer >> 1 & 1);
   if (nw == 2) return warp ^ (layer & 1) << 1;
   return warp;
 }
 
 // What both kernels' chain warps begin with
-#define CHAIN_BEGIN(tensor, stride, back)                                                                                                     \
+#define CHAIN_BEGIN(tensor, stride, back, apart)                                                                                               \
   extern __shared__ __align__(128) unsigned char smem[];                                                                                      \
   __shared__ ChainBars bars;                                                                                                                  \
-  const int nw = a.nw, warp = chain_role(a, nw), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;                                         \
+  const int nw = a.nw, users = (apart) ? 2 * nw : nw, warp = chain_role(a, nw, apart), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;                                         \
   if (threadIdx.x == 0) {                                                                                                                     \
-    for (int i = 0; i < stages; ++i) { mbar_init(bars.full + i, 33); mbar_init(bars.empty + i, nw); }                                         \
+    for (int i = 0; i < stages; ++i) { mbar_init(bars.full + i, 33); mbar_init(bars.empty + i, users); }                                      \
+    for (int i = 0; i < 8; ++i) { mbar_init(bars.ready + i, 1); mbar_init(bars.taken + i, 1); }                                               \
     fence_mbar_init();                                                                                                                        \
   }                                                                                                                                           \
   begin_dependent();                                                                                                                          \
@@ -330,22 +336,123 @@ __device__ __forceinline__ int chain_role(const DeltaArgs &a, int nw) {
   const ChainWork w = chain_work<PACKED>(a, smem);                                                                                            \
   const DeltaSpan sp = delta_span<C>(a, w.b);                                                                                                 \
   const uint32_t ring = smem_u32(smem), sb = (uint32_t)stage_bytes(K, nw);                                                                    \
-  if (warp > nw) return;                                                                                                                      \
-  if (warp == nw) {                                                                                                                           \
+  if (warp > users) return;                                                                                                                   \
+  if (warp == users) {                                                                                                                        \
     chain_fill<K>(a, w, sp, tensor, stride, nw, stages, ring, bars.full, bars.empty, lane, back);                                             \
     return;                                                                                                                                   \
   }                                                                                                                                           \
-  const int n = w.n, v0 = 16 * (w.slab * nw + warp), V = a.V, pv = pitch_v(nw);                                                               \
+  const int mine = warp < nw ? warp : warp - nw, n = w.n, v0 = 16 * (w.slab * nw + mine), V = a.V, pv = pitch_v(nw);                          \
   const Lanes l(lane);                                                                                                                        \
   const uint32_t v_off = 2 * C * pitch_k(K), r_off = v_off + C * pv;                                                                          \
-  const uint32_t v_at = v_off + 32 * warp + (l.row + 8 * l.mat_hi) * pv + 16 * l.mat_lo, v_mine = v_off + 32 * warp + lane * pv;                \
+  const uint32_t v_at = v_off + 32 * mine + (l.row + 8 * l.mat_hi) * pv + 16 * l.mat_lo, v_mine = v_off + 32 * mine + lane * pv;              \
   const size_t st_at = ((size_t)w.b * a.N + n) * K * V + v0
 
-// Y: y is asked for; KEEP: states and updates are kept for the gradient
-template <int K, bool Y, bool KEEP, bool PACKED>
-__global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, int stages) {
-  CHAIN_BEGIN(a.v, a.vs, false);
-  const uint32_t out = ring + stages * sb + warp * out_bytes(K), spare = ring + stages * sb + nw * out_bytes(K) - v_off;      // (spare: as if a stage, its columns of V)
+// Where a chain finds things in a stage
+struct ChainAt { uint32_t v_at, v_mine, r_off; int pv, c; };
+// X from K S, as operands; T
+__device__ __forceinline__ void x_of(const ChainAt &t, const Lanes &l, uint32_t stage, float (&acc)[4][4], uint32_t (&A)[2][4], uint32_t (&T)[3][4]) {
+  const uint32_t vec = stage + t.r_off + kRecVec + 8 * t.c;
+  uint32_t vt[2][4];
+  rows_in(vt, stage + t.v_at, t.pv);
+  lower_t_in(T, stage + t.r_off + kRecT, l);
+#pragma unroll
+  for (int nt = 0; nt < 4; ++nt) {
+    const float2 e = lds64(vec + 128 * kVecEgk + 32 * nt), b = lds64(vec + 128 * kVecBeta + 32 * nt);
+    const float2 x0 = unpack_bf16(vt[nt >> 1][2 * (nt & 1)]), x1 = unpack_bf16(vt[nt >> 1][2 * (nt & 1) + 1]);
+    acc[nt][0] = b.x * fmaf(-e.x, acc[nt][0], x0.x);
+    acc[nt][1] = b.y * fmaf(-e.y, acc[nt][1], x0.y);
+    acc[nt][2] = b.x * fmaf(-e.x, acc[nt][2], x1.x);
+    acc[nt][3] = b.y * fmaf(-e.y, acc[nt][3], x1.y);
+  }
+  pack_a<4>(acc, 0, A[0]);
+  pack_a<4>(acc, 1, A[1]);
+}
+// Y from q S: scaled, + P U
+__device__ __forceinline__ void y_rest(const ChainAt &t, const Lanes &l, uint32_t stage, float (&y)[4][4], const uint32_t (&Ub)[2][4]) {
+  uint32_t P[3][4];
+  lower_t_in(P, stage + t.r_off + kRecP, l);
+#pragma unroll
+  for (int nt = 0; nt < 4; ++nt) {
+    const float2 e = lds64(stage + t.r_off + kRecVec + 8 * t.c + 128 * kVecEq + 32 * nt);
+    y[nt][0] *= e.x; y[nt][1] *= e.y; y[nt][2] *= e.x; y[nt][3] *= e.y;
+  }
+  mul_lower_t(y, Ub, P);
+}
+// Where a chunk's U has what is not finite, before its Y: U once more from the S that Y is going to read (operand kt: s_of), and y begun with
+// NaN from the first such token on.
+template <int K, typename F>
+__device__ __forceinline__ void mend(const ChainAt &t, const Lanes &l, uint32_t stage, F s_of, uint32_t (&Ub)[2][4], float (&y)[4][4]) {
+  RowsT<K> kb;
+  kb.start(stage, l);
+  float acc[4][4], U[4][4];
+  zero(acc);
+#pragma unroll
+  for (int kt = 0; kt < K / 16; ++kt) {
+    uint32_t f[4];
+    s_of(kt, f);
+    kb.step(acc, f, kt);
+  }
+  uint32_t A[2][4], T[3][4];
+  x_of(t, l, stage, acc, A, T);
+  const FirstOdd x = take_odd(A, t.c);
+  zero(U);
+  mul_lower_t(U, A, T);
+  pack_a<4>(U, 0, Ub[0]);
+  pack_a<4>(U, 1, Ub[1]);
+  const FirstOdd u = take_odd(Ub, t.c);      // (T's rows may have such entries where X has none)
+#pragma unroll
+  for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (8 * nt + 2 * t.c + (r & 1) >= min(x.at[r >> 1], u.at[r >> 1])) y[nt][r] = __int_as_float(0x7fffffff);
+}
+
+// Y: y is asked for; KEEP: states and updates are kept for the gradient; APART: Y is a warp's of its own, beside each chain (1: up to two of
+// these, seven warps at most; 2: four, nine warps, which leaves a thread fewer registers)
+template <int K, bool Y, bool KEEP, bool PACKED, int APART>
+__global__ void __launch_bounds__(APART == 2 ? 288 : APART ? 224 : 160, APART ? 1 : 2) delta_chain_fwd_kernel(DeltaArgs a, int stages) {
+  CHAIN_BEGIN(a.v, a.vs, false, APART != 0);
+  const ChainAt t{v_at, v_mine, r_off, pv, c};
+  constexpr bool WITH = Y && !APART;      // the chain does Y too
+  const uint32_t out = ring + stages * sb + (APART ? 2 * mine * apart_bytes(K) : warp * out_bytes(K));
+  const uint32_t spare = ring + stages * sb + nw * out_bytes(K) - v_off;      // (as if a stage, its columns of V)
+  const uint32_t s_lane = 16 * l.row + 128 * (l.mat_lo * (K / 8) + l.mat_hi), u_lane = 32 * K + 16 * l.row + 128 * (4 * l.mat_lo + l.mat_hi);      // blocks [column tile][tile]
+  __nv_bfloat16 *yg = Y ? static_cast<__nv_bfloat16 *>(a.y) + ((size_t)(sp.tok0 + lane) * a.N + n) * V + v0 : nullptr;
+  if (APART && warp >= nw) {      // S and U of chunk after chunk from the chain's two buffers
+    int st = 0;
+    uint32_t phase = 0;
+    for (int ch = 0; ch < sp.n; ++ch) {
+      const int buf = 2 * mine + (ch & 1);
+      if (!mbar_wait(bars.full + st, phase) || !mbar_wait(bars.ready + buf, (ch >> 1) & 1)) {
+        if (lane == 0) report_timeout(a.dev_status);
+        return;
+      }
+      const uint32_t stage = ring + st * sb, at = out + (ch & 1) * apart_bytes(K);
+      RowsT<K> qb;
+      qb.start(stage + C * pitch_k(K), l);
+      uint32_t Ub[2][4], f[2][4];
+      ldmatrix_x4(at + u_lane, Ub[0]);
+      ldmatrix_x4(at + u_lane + 256, Ub[1]);
+      ldmatrix_x4(at + s_lane, f[0]);
+      float y[4][4];
+      zero(y);
+      if (any_odd(Ub)) mend<K>(t, l, stage, [&](int kt, uint32_t (&x)[4]) { ldmatrix_x4(at + s_lane + 256 * kt, x); }, Ub, y);
+#pragma unroll
+      for (int kt = 0; kt < K / 16; ++kt) {
+        if (kt + 1 < K / 16) ldmatrix_x4(at + s_lane + 256 * (kt + 1), f[(kt + 1) & 1]);
+        qb.step(y, f[kt & 1], kt);
+      }
+      y_rest(t, l, stage, y, Ub);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bars.taken + buf);
+      rows_out(y, stage + v_at, stage + v_mine, pv, yg, lane < sp.T - ch * C);      // (through V's place: the chain has read it)
+      yg += (size_t)C * a.N * V;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bars.empty + st);
+      if (++st == stages) { st = 0; phase ^= 1; }
+    }
+    return;
+  }
   float S[K / 8][4];
   if (a.h0) state_in<K>(S, a.h0, st_at, a.state_bf16, V, g, c);
   else
@@ -353,105 +460,51 @@ __global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, in
     for (int nt = 0; nt < K / 8; ++nt)
 #pragma unroll
       for (int r = 0; r < 4; ++r) S[nt][r] = 0.f;
-  __nv_bfloat16 *yg = Y ? static_cast<__nv_bfloat16 *>(a.y) + ((size_t)(sp.tok0 + lane) * a.N + n) * V + v0 : nullptr;
   char *sg = KEEP ? a.states + ((size_t)sp.slot0 * a.N + n) * (2 * K * V) + 2 * K * v0 + 4 * lane : nullptr, *ug = KEEP ? a.upd + ((size_t)sp.slot0 * a.N + n) * (2 * C * V) + 2 * C * v0 + 4 * lane : nullptr;
-  const uint32_t s_at = out + 16 * l.row + 128 * (l.mat_lo * (K / 8) + l.mat_hi);      // tiles of S: 256 bytes apart
+  const uint32_t s_at = out + s_lane;      // tiles of S: 256 bytes apart
   uint32_t Ub[2][4] = {}, Sb[K <= 64 ? K / 16 : 1][4] = {};      // U, S as operands
   float y[4][4];
-  // Y from q S: scaled, + P U
-  auto y_rest = [&](uint32_t stage) {
-    uint32_t P[3][4];
-    lower_t_in(P, stage + r_off + kRecP, l);
-#pragma unroll
-    for (int nt = 0; nt < 4; ++nt) {
-      const float2 e = lds64(stage + r_off + kRecVec + 8 * c + 128 * kVecEq + 32 * nt);
-      y[nt][0] *= e.x; y[nt][1] *= e.y; y[nt][2] *= e.x; y[nt][3] *= e.y;
-    }
-    mul_lower_t(y, Ub, P);
-  };
-  // X from K S, as operands; T
-  auto x_of = [&](uint32_t stage, float (&acc)[4][4], uint32_t (&A)[2][4], uint32_t (&T)[3][4]) {
-    const uint32_t vec = stage + r_off + kRecVec + 8 * c;
-    uint32_t vt[2][4];
-    rows_in(vt, stage + v_at, pv);
-    lower_t_in(T, stage + r_off + kRecT, l);
-#pragma unroll
-    for (int nt = 0; nt < 4; ++nt) {
-      const float2 e = lds64(vec + 128 * kVecEgk + 32 * nt), b = lds64(vec + 128 * kVecBeta + 32 * nt);
-      const float2 x0 = unpack_bf16(vt[nt >> 1][2 * (nt & 1)]), x1 = unpack_bf16(vt[nt >> 1][2 * (nt & 1) + 1]);
-      acc[nt][0] = b.x * fmaf(-e.x, acc[nt][0], x0.x);
-      acc[nt][1] = b.y * fmaf(-e.y, acc[nt][1], x0.y);
-      acc[nt][2] = b.x * fmaf(-e.x, acc[nt][2], x1.x);
-      acc[nt][3] = b.y * fmaf(-e.y, acc[nt][3], x1.y);
-    }
-    pack_a<4>(acc, 0, A[0]);
-    pack_a<4>(acc, 1, A[1]);
-  };
-  // Where a chunk's U has what is not finite, before its Y: U once more from the S that Y is going to read, and y begun with NaN from the first
-  // such token on.
   bool odd = false;
-  auto mend = [&](uint32_t stage) {
-    RowsT<K> kb;
-    kb.start(stage, l);
-    float acc[4][4], U[4][4];
-    zero(acc);
+  // operand kt of the S that Y reads
+  auto s_of = [&](int kt, uint32_t (&f)[4]) {
+    if constexpr (K > 64) ldmatrix_x4(s_at + 256 * kt, f);
+    else {
 #pragma unroll
-    for (int kt = 0; kt < K / 16; ++kt) {
-      if constexpr (K > 64) {
-        uint32_t f[4];
-        ldmatrix_x4(s_at + 256 * kt, f);
-        kb.step(acc, f, kt);
-      } else {
-        kb.step(acc, Sb[kt], kt);
-      }
+      for (int r = 0; r < 4; ++r) f[r] = Sb[kt][r];
     }
-    uint32_t A[2][4], T[3][4];
-    x_of(stage, acc, A, T);
-    const FirstOdd x = take_odd(A, c);
-    zero(U);
-    mul_lower_t(U, A, T);
-    pack_a<4>(U, 0, Ub[0]);
-    pack_a<4>(U, 1, Ub[1]);
-    const FirstOdd u = take_odd(Ub, c);      // (T's rows may have such entries where X has none)
-#pragma unroll
-    for (int nt = 0; nt < 4; ++nt)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (8 * nt + 2 * c + (r & 1) >= min(x.at[r >> 1], u.at[r >> 1])) y[nt][r] = __int_as_float(0x7fffffff);
   };
-  // One pass works on a chunk's chain and on the chunk before's Y.  (The first pass's Y is made of what there is, and not stored.)
+  // One pass works on a chunk's chain and (WITH) on the chunk before's Y.  (The first pass's Y is made of what there is, and not stored.)
   int st = 0, before = 0;
   uint32_t phase = 0;
   bool ready = sp.n > 0 && mbar_try_wait(bars.full, 0);
   for (int ch = 0; ch < sp.n; ++ch) {
-    if (!__all_sync(0xffffffffu, ready) && !mbar_wait(bars.full + st, phase)) {
+    const int buf = 2 * mine + (ch & 1);
+    if ((!__all_sync(0xffffffffu, ready) && !mbar_wait(bars.full + st, phase)) || (APART && ch > 1 && !mbar_wait(bars.taken + buf, ((ch >> 1) - 1) & 1))) {
       if (lane == 0) report_timeout(a.dev_status);
       return;
     }
-    const uint32_t stage = ring + st * sb, last = ring + before * sb, vec = stage + r_off + kRecVec + 8 * c;
+    const uint32_t stage = ring + st * sb, last = ring + before * sb, vec = stage + r_off + kRecVec + 8 * c, to = APART ? s_at + (ch & 1) * apart_bytes(K) : s_at;
     zero(y);
-    if (Y && odd) mend(last);
+    if (WITH && odd) mend<K>(t, l, last, s_of, Ub, y);
     RowsT<K> kb, qb;
     kb.start(stage, l);
-    if (Y) qb.start(last + C * pitch_k(K), l);
+    if (WITH) qb.start(last + C * pitch_k(K), l);
     const float ec = __expf(lds32(stage + r_off + kRecVec + 128 * kVecG + 124));
     float acc[4][4];
     zero(acc);
     uint32_t fo[2][4];      // the chunk before's S
-    if (Y && K > 64) ldmatrix_x4(s_at, fo[0]);
+    if (WITH && K > 64) ldmatrix_x4(s_at, fo[0]);
 #pragma unroll
     for (int kt = 0; kt < K / 16; ++kt) {
       uint32_t f[4];
       pack_a<K / 8>(S, kt, f);
-      if (Y && K > 64) {
-        if (kt + 1 < K / 16) ldmatrix_x4(s_at + 256 * (kt + 1), fo[(kt + 1) & 1]);
-        stmatrix_x4(s_at + 256 * kt, f);
-      }
+      if (WITH && K > 64 && kt + 1 < K / 16) ldmatrix_x4(s_at + 256 * (kt + 1), fo[(kt + 1) & 1]);
+      if (APART || (WITH && K > 64)) stmatrix_x4(to + 256 * kt, f);
       if (KEEP) blocks_to(f, sg, K / 8, kt);
 #pragma unroll
       for (int r = 0; r < 4; ++r) { S[2 * kt][r] *= ec; S[2 * kt + 1][r] *= ec; }
       kb.step(acc, f, kt);
-      if (Y) {
+      if (WITH) {
         if constexpr (K > 64) {
           qb.step(y, fo[kt & 1], kt);
         } else {
@@ -461,9 +514,9 @@ __global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, in
         }
       }
     }
-    if (Y) y_rest(last);
+    if (WITH) y_rest(t, l, last, y, Ub);
     uint32_t A[2][4], T[3][4];
-    x_of(stage, acc, A, T);
+    x_of(t, l, stage, acc, A, T);
     float U[4][4];
     zero(U);
     mul_lower_t(U, A, T);
@@ -472,6 +525,7 @@ __global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, in
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       pack_a<4>(U, kt, Ub[kt]);
+      if (APART) stmatrix_x4(out + (ch & 1) * apart_bytes(K) + u_lane + 256 * kt, Ub[kt]);
       if (KEEP) blocks_to(Ub[kt], ug, 4, kt);
 #pragma unroll
       for (int nt = 2 * kt; nt < 2 * kt + 2; ++nt) {
@@ -485,36 +539,37 @@ __global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, in
     ready = ch + 1 < sp.n && mbar_try_wait(bars.full + next, next_phase);
     // S'
     rb.run(S, A);
-    if (Y) {
+    if (WITH) {
       odd = any_odd(Ub);
       const uint32_t y_to = ch > 0 ? last : spare;      // (through V's place, which has been read)
       rows_out(y, y_to + v_at, y_to + v_mine, pv, yg, ch > 0);
       if (ch > 0) yg += (size_t)C * a.N * V;
     }
     __syncwarp();
-    if (lane == 0 && ch > 0) mbar_arrive(bars.empty + before);      // (a chunk's stage is Y's too, a chunk later)
+    if (WITH) {
+      if (lane == 0 && ch > 0) mbar_arrive(bars.empty + before);      // (a chunk's stage is Y's too, a chunk later)
+    } else if (lane == 0) {
+      if (APART) mbar_arrive(bars.ready + buf);
+      mbar_arrive(bars.empty + st);
+    }
     if (KEEP) { sg += (size_t)a.N * (2 * K * V); ug += (size_t)a.N * (2 * C * V); }
     before = st;
     st = next;
     phase = next_phase;
   }
-  if (Y && sp.n > 0) {
+  if (WITH && sp.n > 0) {
     const uint32_t last = ring + before * sb;
     zero(y);
-    if (odd) mend(last);
+    if (odd) mend<K>(t, l, last, s_of, Ub, y);
     RowsT<K> qb;
     qb.start(last + C * pitch_k(K), l);
 #pragma unroll
     for (int kt = 0; kt < K / 16; ++kt) {
-      if constexpr (K > 64) {
-        uint32_t f[4];
-        ldmatrix_x4(s_at + 256 * kt, f);
-        qb.step(y, f, kt);
-      } else {
-        qb.step(y, Sb[kt], kt);
-      }
+      uint32_t f[4];
+      s_of(kt, f);
+      qb.step(y, f, kt);
     }
-    y_rest(last);
+    y_rest(t, l, last, y, Ub);
     rows_out(y, last + v_at, last + v_mine, pv, yg, lane < sp.T - (sp.n - 1) * C);
   }
   if (a.hT) state_out<K>(S, a.hT, st_at, a.state_bf16, V, g, c);
@@ -522,7 +577,7 @@ __global__ void __launch_bounds__(160, 2) delta_chain_fwd_kernel(DeltaArgs a, in
 
 template <int K, bool PACKED>
 __global__ void __launch_bounds__(160, 2) delta_chain_bwd_kernel(DeltaArgs a, int stages) {
-  CHAIN_BEGIN(a.dy, (long long)a.N * a.V, true);
+  CHAIN_BEGIN(a.dy, (long long)a.N * a.V, true, false);
   float S[K / 8][4];    // dS
   if (a.d_hT) state_in<K>(S, a.d_hT, st_at, a.state_bf16, V, g, c);
   else
@@ -621,11 +676,11 @@ __global__ void __launch_bounds__(160, 2) delta_chain_bwd_kernel(DeltaArgs a, in
 
 // 16-column warps of a CTA: four (they share the copies of k, q and the records), two or one where that leaves a quarter fewer chains to
 // the SM that has the most: chains of an SM share its shared memory's bandwidth (65 536 tokens, 32 heads of 128 x 128: 64 CTAs of four
-// 2 354 us, 128 of two 1 576).
-ChainPlan plan_chain(const DeltaArgs &a) {
+// 2 354 us, 128 of two 1 576, both with Y in the chains).
+ChainPlan plan_chain(const DeltaArgs &a, bool with_y) {
   const int cols = a.V / 16;
   const long long units = (long long)a.B * a.N, sms = sm_count();
-  ChainPlan p{1, 1, 4, 0};
+  ChainPlan p{1, 1, 4, 0, 0};
   long long least = 0;
   for (int nw = cols < 4 ? cols : 4; nw >= 1; nw /= 2) {
     const long long chains = (units * (cols / nw) + sms - 1) / sms * nw;
@@ -635,21 +690,29 @@ ChainPlan plan_chain(const DeltaArgs &a) {
   // Two CTAs to an SM where there are that many, but above K = 64 one: four chains of K = 128 take 1.5 us a chunk, eight 2.9, and a batch
   // is done no sooner than its longest sequence (12 of up to 4 000 tokens, 16 heads: 370 us with two, 266 with one).
   const bool one = a.K > 64;
-  const size_t room = (size_t)(!one && units * p.slabs > sms ? 113 : 226) * 1024, fixed = (size_t)p.nw * out_bytes(a.K) + C * pitch_v(p.nw), sb = (size_t)stage_bytes(a.K, p.nw);
+  // Y in warps of their own where a chain has a scheduler to itself, or an SM only one CTA: 2 001 tokens of 84 heads of 128 x 16 52 -> 40 us, of
+  // 64 x 16 with the states kept 36 -> 31, of 32 heads of 128 x 128 (two to an SM) 54 -> 49, the ragged batch of 128 x 128 (four) 270 -> 242;
+  // but four chains of 64 x 64 49.5 -> 55.7, and of K = 16 20.9 -> 22.8.
+  p.apart = !with_y ? 0 : p.nw == 4 ? (one ? 2 : 0) : one || (a.K > 16 && units * p.slabs <= sms) ? 1 : 0;
+  const size_t room = (size_t)(!one && units * p.slabs > sms ? 113 : 226) * 1024, fixed = p.apart ? (size_t)p.nw * 2 * apart_bytes(a.K) : (size_t)p.nw * out_bytes(a.K) + C * pitch_v(p.nw), sb = (size_t)stage_bytes(a.K, p.nw);
   while (p.stages > 3 && fixed + p.stages * sb > room) --p.stages;
   p.smem = std::max(fixed + p.stages * sb, one ? (size_t)115 * 1024 : 0);
   return p;
 }
 
+template <int K, bool PACKED, int APART> auto fwd_kernel(bool keep) {
+  return keep ? delta_chain_fwd_kernel<K, true, true, PACKED, APART> : delta_chain_fwd_kernel<K, true, false, PACKED, APART>;
+}
 template <int K, bool PACKED> cudaError_t launch_kp(const DeltaArgs &args, bool backward, cudaStream_t s) {
   DeltaArgs a = args;
-  const ChainPlan p = plan_chain(a);
+  const ChainPlan p = plan_chain(a, !backward && a.y);
   a.nw = p.nw; a.sms = sm_count();
-  void (*kernel)(DeltaArgs, int) = backward ? delta_chain_bwd_kernel<K, PACKED> : !a.states ? delta_chain_fwd_kernel<K, true, false, PACKED>
-                                   : a.y ? delta_chain_fwd_kernel<K, true, true, PACKED> : delta_chain_fwd_kernel<K, false, true, PACKED>;
+  void (*kernel)(DeltaArgs, int) = backward ? delta_chain_bwd_kernel<K, PACKED> : !a.y ? delta_chain_fwd_kernel<K, false, true, PACKED, 0>
+                                   : p.apart == 0 ? fwd_kernel<K, PACKED, 0>(a.states) : p.apart == 1 ? fwd_kernel<K, PACKED, 1>(a.states)
+                                                                                                     : fwd_kernel<K, PACKED, (K > 64 ? 2 : 1)>(a.states);
   const cudaError_t e = allow_smem(kernel, p.smem);
   if (e != cudaSuccess) return e;
-  return launch_early(kernel, dim3((unsigned)((long long)a.B * a.N * p.slabs)), dim3(p.nw == 2 ? 128 : 32 * (p.nw + 1)), p.smem, s, a, p.stages);
+  return launch_early(kernel, dim3((unsigned)((long long)a.B * a.N * p.slabs)), dim3(p.apart ? (p.nw == 2 ? 224 : 32 * (2 * p.nw + 1)) : p.nw == 2 ? 128 : 32 * (p.nw + 1)), p.smem, s, a, p.stages);
 }
 template <int K> cudaError_t launch_k(const DeltaArgs &a, bool backward, cudaStream_t s) {
   return a.cu ? launch_kp<K, true>(a, backward, s) : launch_kp<K, false>(a, backward, s);

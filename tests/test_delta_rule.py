@@ -149,6 +149,33 @@ def test_jobs_of_the_gradient_kernel(B, N, K, V):
     assert max(errs.values()) <= TOL[BF], errs
 
 
+@pytest.mark.parametrize("use_ckpt", [True, False])
+@pytest.mark.parametrize("N,K", [(3, 64), (60, 64), (148, 64), (3, 80), (60, 80), (148, 80)])
+def test_numbers_of_chains(N, K, use_ckpt):
+    """One, two and four chains to an SM, with y from the chains' own warps and from others."""
+    errs = run_both(seed=17, B=1, T=40, N=N, K=K, V=64, Nq=1, Nk=1, use_ckpt=use_ckpt)
+    assert max(errs.values()) <= TOL[BF], errs
+
+
+@pytest.mark.parametrize("N,K", [(60, 64), (148, 64), (60, 80), (148, 80)])
+def test_numbers_of_chains_and_a_value_that_is_not_finite(N, K):
+    x, on, H0, dy, d_hT, o = make(18, B=1, T=75, N=N, K=K, V=64, gate="log", step="value")
+    o = on_gpu(o)
+    want = m.m2rnn_delta_fwd(*on, H0.cuda(), **o)[0]
+    for at in (0, 20, 31, 40, 74):
+        for which in (1, 2):
+            bad = [t.clone() for t in on]
+            bad[which][0, at, 1, 9] = math.nan
+            for save in (False, True):
+                y = m.m2rnn_delta_fwd(*bad, H0.cuda(), save_ckpt=save, **o)[0]
+                others = [n for n in range(N) if n != 1]
+                assert torch.equal(y[0][:, others], want[0][:, others])
+                cols = slice(None) if which == 1 else slice(9, 10)
+                assert torch.isnan(y[0, at:, 1, cols]).all()
+                if at:
+                    assert rel(y[0, :at, 1], want[0, :at, 1].cpu()) <= TOL[BF]
+
+
 def test_keys_that_point_the_same_way():
     """T's diagonal blocks by substitution: with equal keys and steps of 1 M is a triangle of ones."""
     x, on, H0, dy, d_hT, o = make(8, B=1, T=96, N=2, K=64, V=32, gate="log", step="value")
