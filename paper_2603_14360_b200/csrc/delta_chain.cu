@@ -19,7 +19,7 @@
 // the chains to an SM.)  What is kept for the gradient goes from registers to memory, 128 bytes an instruction.
 // Roundings to bf16: the operands S, X, U (dS, dU, L), the factored e^(g_last - g) U and the like, and T and P.  S itself
 // is held and updated in fp32.
-// Bound by the chain's latency where an SM has a chain to a scheduler (1 001 tokens, 84 heads of 64 x 16: 15.9 us, 0.45 a chunk; 65 536 tokens,
+// Bound by the chain's latency where an SM has a chain to a scheduler (1 001 tokens, 84 heads of 64 x 16: 16.1 us, 0.45 a chunk; 65 536 tokens,
 // 32 heads of 128 x 128, two chains to an SM: 1 383 us, 0.68 a chunk; 8 x 2 048 tokens, 16 heads of 64 x 64, four: 49.5 us, 0.77), by shared memory's
 // bandwidth where it has more (two to a scheduler: LSU data pipe 83 % busy).
 #include <algorithm>
@@ -310,12 +310,13 @@ __device__ __forceinline__ void rows_out(const float (&x)[4][4], uint32_t at, ui
 // Barriers of a CTA: stages filled and free; a chain's S and U there for its Y's warp, and taken
 struct ChainBars { uint64_t full[8], empty[8], ready[8], taken[8]; };      // (ready, taken: two buffers of a chain)
 
-// A warp's part: 0 .. nw - 1 a chain, nw copies, above that none; apart: nw .. 2 nw - 1 the chains' Y, 2 nw copies.  An SM's CTAs come a layer after the other, and warp w of the SM's
+// A warp's part: 0 .. nw - 1 a chain, nw copies, above that none; apart: nw .. 2 nw - 1 the chains' Y, 2 nw copies (with one chain the middle
+// warp, with two the seventh, the fifth and sixth doing nothing: so that chains and Y have schedulers of their own, of two CTAs too).  An SM's CTAs come a layer after the other, and warp w of the SM's
 // belongs to scheduler w % 4: with CTAs of two warps (a chain) or four (two) the parts of every second pair of layers, or layer, change
 // places, so that chains share a scheduler only where there are more than four to the SM.
 __device__ __forceinline__ int chain_role(const DeltaArgs &a, int nw, bool apart) {
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), layer = (int)(blockIdx.x / (unsigned)a.sms);
-  if (apart) return nw == 2 && warp >= 4 ? (warp == 6 ? 4 : 5) : warp;
+  if (apart) return nw == 1 ? (3 - warp) % 3 : nw == 2 && warp >= 4 ? (warp == 6 ? 4 : 5) : warp;
   if (nw == 1) return warp ^ (layer >> 1 & 1);
   if (nw == 2) return warp ^ (layer & 1) << 1;
   return warp;
@@ -690,11 +691,14 @@ ChainPlan plan_chain(const DeltaArgs &a, bool with_y) {
   // Two CTAs to an SM where there are that many, but above K = 64 one: four chains of K = 128 take 1.5 us a chunk, eight 2.9, and a batch
   // is done no sooner than its longest sequence (12 of up to 4 000 tokens, 16 heads: 370 us with two, 266 with one).
   const bool one = a.K > 64;
-  // Y in warps of their own where a chain has a scheduler to itself, or an SM only one CTA: 2 001 tokens of 84 heads of 128 x 16 52 -> 40 us, of
-  // 64 x 16 with the states kept 36 -> 31, of 32 heads of 128 x 128 (two to an SM) 54 -> 49, the ragged batch of 128 x 128 (four) 270 -> 242;
-  // but four chains of 64 x 64 49.5 -> 55.7, and of K = 16 20.9 -> 22.8.
-  p.apart = !with_y ? 0 : p.nw == 4 ? (one ? 2 : 0) : one || (a.K > 16 && units * p.slabs <= sms) ? 1 : 0;
-  const size_t room = (size_t)(!one && units * p.slabs > sms ? 113 : 226) * 1024, fixed = p.apart ? (size_t)p.nw * 2 * apart_bytes(a.K) : (size_t)p.nw * out_bytes(a.K) + C * pitch_v(p.nw), sb = (size_t)stage_bytes(a.K, p.nw);
+  const long long per = (units * p.slabs + sms - 1) / sms;
+  // Y in warps of their own where an SM has one CTA, or up to four of one chain (2 001 tokens a sequence, us without and with): 84 heads of 128 x 16
+  // 52, 40; 32 heads of 128 x 128 (two chains to an SM) 54, 49; the ragged batch of 128 x 128 (four) 270, 242; 84 heads of 64 x 16, 1 sequence 34,
+  // 29, with the states kept 36, 31, 2 sequences 46, 43, 4 (three to an SM) 67, 61, 6 (four) 95, 79.  But four chains of 64 x 64 in a CTA 49.5, 55.7, and
+  // K = 16 20.9, 22.8.
+  p.apart = !with_y ? 0 : p.nw == 4 ? (one ? 2 : 0) : one || (a.K > 16 && per <= (p.nw == 1 ? 4 : 1)) ? 1 : 0;
+  const size_t room = (size_t)(226 / (one || per <= 1 ? 1 : p.apart ? (int)per : 2)) * 1024, sb = (size_t)stage_bytes(a.K, p.nw);
+  const size_t fixed = p.apart ? (size_t)p.nw * 2 * apart_bytes(a.K) : (size_t)p.nw * out_bytes(a.K) + C * pitch_v(p.nw);
   while (p.stages > 3 && fixed + p.stages * sb > room) --p.stages;
   p.smem = std::max(fixed + p.stages * sb, one ? (size_t)115 * 1024 : 0);
   return p;

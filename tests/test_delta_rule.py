@@ -157,6 +157,13 @@ def test_numbers_of_chains(N, K, use_ckpt):
     assert max(errs.values()) <= TOL[BF], errs
 
 
+@pytest.mark.parametrize("N", [200, 400, 560, 700])
+@pytest.mark.parametrize("K", [16, 32, 64, 96])
+def test_numbers_of_ctas_of_one_chain(N, K):
+    errs = run_both(seed=19, B=1, T=40, N=N, K=K, V=16, Nq=1, Nk=1)
+    assert max(errs.values()) <= TOL[BF], errs
+
+
 @pytest.mark.parametrize("N,K", [(60, 64), (148, 64), (60, 80), (148, 80)])
 def test_numbers_of_chains_and_a_value_that_is_not_finite(N, K):
     x, on, H0, dy, d_hT, o = make(18, B=1, T=75, N=N, K=K, V=64, gate="log", step="value")
