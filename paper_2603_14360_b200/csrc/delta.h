@@ -26,7 +26,7 @@ enum {
   kVecDlog = 7   // d log a / d gate entry
 };
 constexpr int kRecChain = kRecVec + 4 * 128 + 128;     // what the chains read of it: up to and with kVecG
-constexpr int kRecF32Bytes = (3 * 256 + 8 * 16) * 4;   // fp32: T, P, M 16 x 16, then the vectors
+constexpr int kRecF32Bytes = (3 * 256 + 11 * 16) * 4;   // fp32: T, P, M 16 x 16, then eleven vectors (delta_f32.cu)
 
 struct DeltaArgs {
   int B, T, N, Nq, Nk, K, V;

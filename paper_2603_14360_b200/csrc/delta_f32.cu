@@ -17,8 +17,23 @@ namespace {
 
 constexpr int C = kDeltaChunkF32;
 constexpr int kT = 0, kP = C * C, kM = 2 * C * C, kVec = 3 * C * C, kRec = kRecF32Bytes / 4;      // floats of a record
-static_assert(kVec + 8 * C == kRec && kP == C * C, "");
-enum { kBeta = kVecBeta };
+// a token's factors: of kVec* of delta.h those of the numbers 0 .. 3, 5 and 6, and these.  (The chains copy the first eight arrays.)
+enum {
+  kBeta = kVecBeta,
+  kEg = kVecG,      // e^g
+  kEl = kVecDlog,   // e^(g_last - g)
+  kGHigh = 8, kGLow = 9, kDlog = 10
+};
+static_assert(kVec + 11 * C == kRec && kP == C * C && kEg == 4 && kEl == 7, "");
+
+// Running sums of log a are kept as pairs of floats, kGHigh and what that leaves out (kGLow), and differences of two are taken in 64 bits: a
+// dropped state (kLogFloor) or a strong decay stays in every later sum, and behind sixteen of them a float is 1.2e-4 from the next, where
+// the decay between two tokens needs 2^-24 of itself.  e^d is that of d's nearest float times 1 + what is left of d.
+__device__ __forceinline__ float exp_of(double d) {
+  const float h = (float)d, e = expf(h);
+  return fmaf(e, (float)(d - h), e);
+}
+__device__ __forceinline__ double sum_at(const float *vec, int i) { return (double)vec[C * kGHigh + i] + vec[C * kGLow + i]; }
 
 // ---- prep
 
@@ -50,16 +65,18 @@ __global__ void __launch_bounds__(128) delta_prep_f32_kernel(DeltaArgs a) {
       la = delta_log_decay(a.gate_kind, static_cast<const float *>(a.gate)[at], psi ? a.alpha[n] : 1.f, psi ? a.beta[n] : 0.f, dl);
       bt = delta_step_of(a.step_kind, static_cast<const float *>(a.step)[at], unused);
     }
-    float gs = la;
+    double gs = la;
 #pragma unroll
     for (int d = 1; d < C; d *= 2) {
-      const float o = __shfl_up_sync(0xffffffffu, gs, d);
+      const double o = __shfl_up_sync(0xffffffffu, gs, d);
       if (lane >= d) gs += o;
     }
     if (lane < C) {
-      vec[C * kVecG + lane] = gs;
+      const float high = (float)gs;
+      vec[C * kGHigh + lane] = high;
+      vec[C * kGLow + lane] = (float)(gs - high);
       vec[C * kBeta + lane] = bt;
-      vec[C * kVecDlog + lane] = dl;
+      vec[C * kDlog + lane] = dl;
     }
   }
   cp_wait_all();
@@ -75,10 +92,13 @@ __global__ void __launch_bounds__(128) delta_prep_f32_kernel(DeltaArgs a) {
   __syncthreads();
   float *rec = reinterpret_cast<float *>(a.rec) + ((size_t)(sp.slot0 + ch) * a.N + n) * kRec;
   if (tid < C) {
-    const float gs = vec[C * kVecG + tid], eg = expf(gs), rk = vec[C * kVecRk + tid], rq = vec[C * kVecRq + tid];
+    const double gs = sum_at(vec, tid);
+    const float eg = exp_of(gs), el = exp_of(sum_at(vec, C - 1) - gs), rk = vec[C * kVecRk + tid], rq = vec[C * kVecRq + tid];
     vec[C * kVecEgk + tid] = eg * rk;
     vec[C * kVecEq + tid] = a.scale * eg * rq;
-    vec[C * kVecEk + tid] = expf(vec[C * kVecG + C - 1] - gs) * rk;
+    vec[C * kEg + tid] = eg;
+    vec[C * kEl + tid] = el;
+    vec[C * kVecEk + tid] = el * rk;
   }
   for (int x = tid; x < 2 * C * C; x += 128) {
     const int i = x / C % C, j = x % C;
@@ -92,7 +112,7 @@ __global__ void __launch_bounds__(128) delta_prep_f32_kernel(DeltaArgs a) {
         s0 = fmaf(u.x, w.x, fmaf(u.y, w.y, s0));
         s1 = fmaf(u.z, w.z, fmaf(u.w, w.w, s1));
       }
-      s = (s0 + s1) * expf(vec[C * kVecG + i] - vec[C * kVecG + j]) * vec[C * kVecRk + j] *
+      s = (s0 + s1) * exp_of(sum_at(vec, i) - sum_at(vec, j)) * vec[C * kVecRk + j] *
           (p ? a.scale * vec[C * kVecRq + i] : vec[C * kBeta + i] * vec[C * kVecRk + i]);
     }
     rec[(p ? kP : kM) + i * C + j] = s;
@@ -111,7 +131,7 @@ __global__ void __launch_bounds__(128) delta_prep_f32_kernel(DeltaArgs a) {
 #pragma unroll
     for (int i = 0; i < C; ++i) rec[kT + i * C + tid] = t[i];
   }
-  rec[kVec + tid] = vec[tid];
+  for (int x = tid; x < 11 * C; x += 128) rec[kVec + x] = vec[x];
 }
 
 // ---- chains
@@ -251,7 +271,7 @@ __global__ void __launch_bounds__(288) delta_chain_f32_kernel(DeltaArgs a, int n
     const float *ks = sm + st * f32_stage(K, nc), *qs = ks + C * K, *rec = qs + C * K, *vec = rec + kSVec, *vt = rec + kSRec;
     const long long tok = sp.tok0 + ch * C;
     const size_t slot = (size_t)(sp.slot0 + ch) * a.N + n;
-    const float x0 = vt[l * nc + mine], ec = expf(vec[C * kVecG + C - 1]);
+    const float x0 = vt[l * nc + mine], ec = vec[C * kEg + C - 1];
     float *states = reinterpret_cast<float *>(BWD ? a.dstates : a.states);
     if (states) rows_to<M>(states + slot * K * V + (size_t)v * K + M * l, S);
     if constexpr (!BWD) {
@@ -327,7 +347,7 @@ __global__ void __launch_bounds__(288) delta_chain_f32_kernel(DeltaArgs a, int n
 
 constexpr int kThreads = 256;
 // Shared memory (floats): S, dS' [V][K]; dY, L, U [V][kPM]; k, q [C][K + 1]; five arrays [C][K + 1]; four matrices; the vectors; sums
-__host__ __device__ constexpr int grad_floats(int K, int V) { return 2 * K * V + 3 * V * kPM + 7 * C * (K + 1) + 4 * C * C + 8 * C + 8 * C + 16; }
+__host__ __device__ constexpr int grad_floats(int K, int V) { return 2 * K * V + 3 * V * kPM + 7 * C * (K + 1) + 4 * C * C + 11 * C + 8 * C + 16; }
 static_assert(grad_floats(128, 128) * 4 <= 227 * 1024, "");
 
 __global__ void __launch_bounds__(kThreads) delta_grad_f32_kernel(DeltaArgs a) {
@@ -343,7 +363,7 @@ __global__ void __launch_bounds__(kThreads) delta_grad_f32_kernel(DeltaArgs a) {
   const int have = min(C, sp.T - ch * C);
   const size_t slot = (size_t)(sp.slot0 + ch) * a.N + n;
   float *S = sm, *D = S + K * V, *yt = D + K * V, *lt = yt + V * kPM, *ut = lt + V * kPM;
-  float *XP = ut + V * kPM, *XPt = XP + C * C, *XN = XPt + C * C, *XNt = XN + C * C, *vec = XNt + C * C, *sums = vec + 8 * C;
+  float *XP = ut + V * kPM, *XPt = XP + C * C, *XN = XPt + C * C, *XNt = XN + C * C, *vec = XNt + C * C, *sums = vec + 11 * C;
   float *ks = sums + 8 * C + 16, *qs = ks + C * PK, *m0 = qs + C * PK;      // five arrays from m0: dQ^, dK-, dK+, and R's and W's parts
   const float *rec = reinterpret_cast<const float *>(a.rec) + slot * kRec;
   {
@@ -352,7 +372,7 @@ __global__ void __launch_bounds__(kThreads) delta_grad_f32_kernel(DeltaArgs a) {
       cp16(smem_u32(S + 4 * x), sg + 4 * x);
       cp16(smem_u32(D + 4 * x), dg + 4 * x);
     }
-    if (tid < 2 * C) cp16(smem_u32(vec + 4 * tid), rec + kVec + 4 * tid);
+    if (tid < 11 * C / 4) cp16(smem_u32(vec + 4 * tid), rec + kVec + 4 * tid);
     const float *yg = static_cast<const float *>(a.dy) + ((size_t)tok * a.N + n) * V;
     const float *ug = reinterpret_cast<const float *>(a.upd) + slot * C * V, *lg = reinterpret_cast<const float *>(a.lam) + slot * C * V;
     const int log_v = 31 - __clz(V);
@@ -386,7 +406,7 @@ __global__ void __launch_bounds__(kThreads) delta_grad_f32_kernel(DeltaArgs a) {
         p = fmaf(yt[v * kPM + i], ut[v * kPM + j], p);
         m = fmaf(-lt[v * kPM + i], ut[v * kPM + j], m);
       }
-      const float e = expf(vec[C * kVecG + i] - vec[C * kVecG + j]);
+      const float e = exp_of(sum_at(vec, i) - sum_at(vec, j));
       xp = a.scale * e * p;
       if (j < i) {
         xn = e * m;
@@ -428,10 +448,10 @@ __global__ void __launch_bounds__(kThreads) delta_grad_f32_kernel(DeltaArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int i = i0 + e;
-      const float g = vec[C * kVecG + i], eg = expf(g), rk = vec[C * kVecRk + i], rq = vec[C * kVecRq + i];
-      y[e] *= a.scale * eg;
-      ls[e] *= -eg;
-      us[e] *= expf(vec[C * kVecG + C - 1] - g);
+      const float rk = vec[C * kVecRk + i], rq = vec[C * kVecRq + i];
+      y[e] *= a.scale * vec[C * kEg + i];
+      ls[e] *= -vec[C * kEg + i];
+      us[e] *= vec[C * kEl + i];
       m0[3 * AR + i * PK + f] = fmaf(rq * qs[i * PK + f], y[e], vec[C * kBeta + i] * rk * ks[i * PK + f] * ls[e]);
       m0[4 * AR + i * PK + f] = rk * ks[i * PK + f] * us[e];
     }
@@ -495,7 +515,7 @@ __global__ void __launch_bounds__(kThreads) delta_grad_f32_kernel(DeltaArgs a) {
       const size_t x = (size_t)(tok + lane) * a.N + n;
       float db;
       (void)delta_step_of(a.step_kind, static_cast<const float *>(a.step)[x], db);
-      static_cast<float *>(a.dgate)[x] = (part + all + expf(vec[C * kVecG + C - 1]) * sd) * vec[C * kVecDlog + lane];
+      static_cast<float *>(a.dgate)[x] = (part + all + vec[C * kEg + C - 1] * sd) * vec[C * kDlog + lane];
       static_cast<float *>(a.dstep)[x] = (sums[7 * C + lane] + sums[C + lane]) * db;
     }
   }
@@ -540,7 +560,7 @@ template <bool BWD> cudaError_t chain(const DeltaArgs &a, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_delta_fwd_f32(const DeltaArgs &a, cudaStream_t s) {
-  const size_t smem = (size_t)(2 * C * (a.K + 4) + C * (C + 4) + 8 * C) * sizeof(float);
+  const size_t smem = (size_t)(2 * C * (a.K + 4) + C * (C + 4) + 11 * C) * sizeof(float);
   const cudaError_t e = launch_early(delta_prep_f32_kernel, dim3((unsigned)(a.slots * a.N)), dim3(128), smem, s, a);
   return e != cudaSuccess ? e : chain<false>(a, s);
 }
