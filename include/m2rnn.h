@@ -337,6 +337,8 @@ size_t m2rnn_delta_bwd_workspace_bytes(const m2rnn_delta_params *params, int hav
  *        dy [B,T,N,V]; d_hT [B,N,K,V] or NULL
  *   out: dq, dk (summed over the heads that share them), dv, dgate, dstep (w.r.t. the tensors as passed), all dense and
  *        of io_dtype; dh0 or NULL.  Sums are taken in a fixed order: results repeat bit for bit.
+ * Rows of a packed batch's tokens that belong to no sequence (behind the last one, or cut off since a sequence is longer
+ * than T) are left as they are, here and in the forward call's y.
  * The gradients of alpha and beta are elementwise sums of dgate outside the call (d beta_n = sum dgate,
  * d alpha_n = sum dgate softplus(x) / (alpha sigmoid(x)), x = gate + beta_n). */
 int m2rnn_delta_bwd(const m2rnn_delta_params *params, const void *q, const void *k, const void *v, const void *gate,

@@ -19,12 +19,24 @@ __global__ void reduce_dW_kernel(const float *__restrict__ part, float *__restri
 // out[bt][g][:] = sum over the heads n of group g of part[bt][n][:]
 // (Algorithm 2 sums dq and dk over the heads that share them with atomic adds).  Four entries of a row a thread (K is a
 // multiple of 16), eight heads' loads in flight: HBM-bound (one entry and load after another read 71 MB in 19 us, now 14).
-template <typename TIO>
-__global__ void __launch_bounds__(256) reduce_heads_kernel(const float4 *__restrict__ part, TIO *__restrict__ out, size_t rows, int per, int K4) {
+// PACKED: rows of tokens that belong to no sequence, whose parts nobody wrote, are left as they are.
+struct Sequences { const int32_t *cu; int B, T; };
+template <typename TIO, bool PACKED>
+__global__ void __launch_bounds__(256) reduce_heads_kernel(const float4 *__restrict__ part, TIO *__restrict__ out, size_t rows, int per, int K4, int Ng, Sequences q) {
   begin_dependent();
   const size_t x = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (x >= rows * K4) return;
   const size_t row = x / K4, at = row * per * K4 + x % K4;      // row: (bt, g)
+  if constexpr (PACKED) {
+    const long long t = (long long)(row / Ng);
+    int lo = 0, hi = q.B;      // the last sequence that does not begin behind t: lo - 1
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (q.cu[mid] <= t) lo = mid + 1;
+      else hi = mid;
+    }
+    if (lo == 0 || t >= min((long long)q.cu[lo], (long long)q.cu[lo - 1] + q.T)) return;
+  }
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int h0 = 0; h0 < per; h0 += 8) {
     float4 p[8];
@@ -105,13 +117,14 @@ cudaError_t launch_reduce_dW(const float *dW_part, float *dW, int B, int N, int 
 }
 
 cudaError_t launch_reduce_heads(const float *part, void *out, int io_dtype, size_t BT, int N, int Ng,
-                                int K, cudaStream_t s) {
+                                int K, cudaStream_t s, const int32_t *cu, int B, int T) {
   const size_t rows = BT * Ng;
   const int per = N / Ng, K4 = K / 4;
   const unsigned grid = (unsigned)((rows * K4 + 255) / 256);
   const float4 *p = reinterpret_cast<const float4 *>(part);
-  if (io_dtype == M2RNN_F32) (void)launch_early(reduce_heads_kernel<float>, grid, 256, 0, s, p, static_cast<float *>(out), rows, per, K4);
-  else (void)launch_early(reduce_heads_kernel<__nv_bfloat16>, grid, 256, 0, s, p, static_cast<__nv_bfloat16 *>(out), rows, per, K4);
+  const Sequences q{cu, B, T};
+  if (io_dtype == M2RNN_F32) (void)launch_early(cu ? reduce_heads_kernel<float, true> : reduce_heads_kernel<float, false>, grid, 256, 0, s, p, static_cast<float *>(out), rows, per, K4, Ng, q);
+  else (void)launch_early(cu ? reduce_heads_kernel<__nv_bfloat16, true> : reduce_heads_kernel<__nv_bfloat16, false>, grid, 256, 0, s, p, static_cast<__nv_bfloat16 *>(out), rows, per, K4, Ng, q);
   return cudaGetLastError();
 }
 

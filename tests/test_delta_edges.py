@@ -36,3 +36,33 @@ def test_digits_behind_dropped_states(every, drop):
     on = [t.cuda() for t in x]
     errs = forward_and_gradients(x, on, H0, dy, d_hT, o)
     assert max(errs.values()) <= 96 * 2.0 ** -24, errs
+
+
+def packed_with_marks(cu, tokens, most, N, Nq, dtype, seed):
+    """Forward and gradients of a packed batch into buffers full of 3, on workspaces full of NaN, and what was given."""
+    x, on, _, dy, d_hT, o = make(seed, B=len(cu) - 1, T=0, N=N, K=32, V=32, Nq=Nq, Nk=Nq, dtype=dtype, cu=[0, tokens])
+    H0 = torch.randn(len(cu) - 1, N, 32, 32, generator=torch.Generator().manual_seed(seed))
+    more = dict(on_gpu(o), cu_seqlens=torch.tensor(cu, dtype=torch.int32).cuda(), max_seqlen=most, workspace=torch.full((1 << 26,), 0xFF, dtype=torch.uint8).cuda())
+    mark = lambda like: torch.full_like(like, 3.0)  # noqa: E731
+    d_hT = torch.randn(H0.shape, generator=torch.Generator().manual_seed(seed + 1))
+    y, hT, ckpt = m.m2rnn_delta_fwd(*on, H0.cuda(), save_ckpt=True, out=dict(y=mark(on[2])), **more)
+    g = dict(zip(("dq", "dk", "dv", "dgate", "dstep"), map(mark, on)))
+    g = m.m2rnn_delta_bwd(*on, H0.cuda(), dy.cuda(), d_hT.cuda(), ckpt=ckpt, out=g, **more)
+    m.check_device_status()
+    return (x, H0, dy, d_hT, o), dict(y=y, **g), hT
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("Nq", [1, 2, 4])
+@pytest.mark.parametrize("cu,tokens,most", [([0, 30, 77, 90], 100, 47), ([0, 30, 77, 90], 90, 40), ([0, 0, 33, 33], 70, 33)], ids=["behind", "cut", "empty"])
+def test_rows_of_no_sequence_are_left_alone(cu, tokens, most, Nq, dtype):
+    """With q and k shared too, where sums over the heads follow the gradient kernel."""
+    given, out, _ = packed_with_marks(cu, tokens, most, 4, Nq, dtype, 40)
+    rows = torch.zeros(tokens, dtype=torch.bool)
+    for a, b in zip(cu, cu[1:]):
+        rows[a:min(b, a + most)] = True
+    for name, t in out.items():
+        if name != "dh0":
+            t = t.flatten(1).float().cpu()
+            assert (t[~rows] == 3).all(), name
+            assert torch.isfinite(t).all() and not (t[rows] == 3).all(1).any(), name
