@@ -78,11 +78,12 @@ template <int C> __device__ __forceinline__ DeltaSpan delta_span(const DeltaArgs
   return s;
 }
 // The batch entry that chunk slot `slot` belongs to (every lane of a warp calls it): of a packed batch the last one whose slots do not start
-// behind it.  (Jobs are numbered by slots: by entry and chunk of the longest, a ragged batch's were mostly none.)
+// behind it, or entry 0 where none's do (offsets that begin behind 0): whether the slot is one of the entry's is for the caller to see, on both
+// sides (of entry 0's, or of offsets that fall, it may lie before the first).  (Jobs are numbered by slots: by entry and chunk of the longest, a ragged batch's were mostly none.)
 template <int C, bool PACKED> __device__ __forceinline__ int delta_entry(const DeltaArgs &a, unsigned slot) {
   if (!PACKED) return (int)(slot / (unsigned)a.nch);
-  int b = -1;
-  for (int x = 0; x < a.B; x += 32) {
+  int b = 0;
+  for (int x = 1; x < a.B; x += 32) {
     const int i = x + (int)(threadIdx.x & 31);
     const bool in = i < a.B && min(max((long long)a.cu[i], 0ll), a.TT) / C + i <= slot;
     b += __popc(__ballot_sync(0xffffffffu, in));

@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(128) delta_prep_f32_kernel(DeltaArgs a) {
   const int n = (int)(blockIdx.x - at * a.N), b = a.cu ? delta_entry<C, true>(a, at) : delta_entry<C, false>(a, at);
   const DeltaSpan sp = delta_span<C>(a, b);
   const int ch = (int)(at - sp.slot0);
-  if (ch >= sp.n) return;      // (of a packed batch: a slot that is no sequence's)
+  if ((unsigned)ch >= (unsigned)sp.n) return;      // (of a packed batch: a slot that is no sequence's)
   const long long tok = sp.tok0 + ch * C;
   const int have = min(C, sp.T - ch * C);
   float *ks = sm, *qs = ks + C * PK, *Ms = qs + C * PK, *vec = Ms + C * (C + 4);
@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(kThreads) delta_grad_f32_kernel(DeltaArgs a) {
   const int n = (int)(blockIdx.x - at * a.N), b = a.cu ? delta_entry<C, true>(a, at) : delta_entry<C, false>(a, at);
   const DeltaSpan sp = delta_span<C>(a, b);
   const int ch = (int)(at - sp.slot0);
-  if (ch >= sp.n) return;      // (of a packed batch: a slot that is no sequence's)
+  if ((unsigned)ch >= (unsigned)sp.n) return;      // (of a packed batch: a slot that is no sequence's)
   const long long tok = sp.tok0 + ch * C;
   const int have = min(C, sp.T - ch * C);
   const size_t slot = (size_t)(sp.slot0 + ch) * a.N + n;

@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(64 * KG, CTAS) delta_grad_kernel(DeltaArgs a, 
         sp = after;
       }
       const int ch = (int)(slot - sp.slot0);
-      if (ch >= sp.n) continue;
+      if ((unsigned)ch >= (unsigned)sp.n) continue;
       o.tok = sp.tok0 + ch * C;
       o.slot = (size_t)slot * a.N;
       o.have = min(C, sp.T - ch * C);

@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(32 * kWarps, 4) delta_prep_kernel(DeltaArgs a,
   const int n0 = (int)(job - slot * runs) * run, b = delta_entry<kDeltaChunk, PACKED>(a, slot);
   const DeltaSpan sp = delta_span<kDeltaChunk>(a, b);
   const int ch = PACKED ? (int)(slot - sp.slot0) : (int)(slot - (unsigned)b * a.nch);
-  if (ch >= sp.n) return;      // (of a packed batch: a slot that is no sequence's)
+  if ((unsigned)ch >= (unsigned)sp.n) return;      // (of a packed batch: a slot that is no sequence's)
   const long long tok = sp.tok0 + ch * kDeltaChunk;
   const int have = min(kDeltaChunk, sp.T - ch * kDeltaChunk);
   const char *kg = static_cast<const char *>(a.k) + 2 * ((tok + g) * a.ks + (unsigned)n0 / (unsigned)a.per_k * K);

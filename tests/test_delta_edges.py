@@ -66,3 +66,24 @@ def test_rows_of_no_sequence_are_left_alone(cu, tokens, most, Nq, dtype):
             t = t.flatten(1).float().cpu()
             assert (t[~rows] == 3).all(), name
             assert torch.isfinite(t).all() and not (t[rows] == 3).all(1).any(), name
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("Nq", [1, 4])
+@pytest.mark.parametrize("first", [1, 40, 150, 331])
+def test_offsets_that_begin_behind_the_first_token(first, Nq, dtype):
+    """A slice of a larger batch's offsets: those sequences' results, rows of others left alone.  Bounds as in test_delta_rule.
+    (A batch of more tokens than its sequences can have, B times the longest, is refused.)"""
+    cu = [first + c for c in (0, 30, 30, 101, 150)]
+    if first + 170 > 4 * 80:
+        with pytest.raises(m.M2RNNError):
+            packed_with_marks(cu, first + 170, 80, 4, Nq, dtype, 41)
+        return
+    (x, H0, dy, d_hT, o), out, hT = packed_with_marks(cu, first + 170, 80, 4, Nq, dtype, 41)
+    rows = slice(first, cu[-1])
+    y_r, hT_r, g_r = ref.gradients([t[rows].double() for t in x], H0.double(), dy[rows].double(), d_hT.double(), [c - first for c in cu], **o)
+    tol = 2e-2 if dtype == BF else 1e-4
+    assert rel(hT, hT_r) <= tol and rel(out.pop("dh0"), g_r["dh0"]) <= tol
+    for name, t in out.items():
+        assert rel(t[rows], y_r if name == "y" else g_r[name]) <= tol, name
+        assert (t[:first] == 3).all() and (t[cu[-1]:] == 3).all(), name
