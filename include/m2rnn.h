@@ -36,7 +36,8 @@
  *     if one runs out the kernel stores M2RNN_ERR_TIMEOUT there and returns early.
  *     The caller zeroes it and reads it back after synchronising.
  *   - Supported sizes: K a multiple of 16 in 16..128, V in {16,32,64,128}, B,T,N >= 1
- *     (T = 0 or B = 0 is a valid empty call: nothing is launched, hT = h0 is NOT written).
+ *     (T = 0 or B = 0 is a valid empty call: no kernel is launched, and m2rnn_fwd does
+ *     NOT write hT = h0).
  */
 #ifndef M2RNN_H
 #define M2RNN_H
@@ -323,8 +324,8 @@ size_t m2rnn_delta_fwd_workspace_bytes(const m2rnn_delta_params *params, int hav
  *   in : q [B,T,Nq,K], k [B,T,Nk,K], v [B,T,N,V], gate, step [B,T,N]; h0 [B,N,K,V] or NULL (zeros); alpha, beta [N]
  *        fp32 (M2RNN_GATE_PSI only, else ignored)
  *   out: y [B,T,N,V]; hT [B,N,K,V] or NULL; ckpt or NULL
- * T = 0, B = 0 and a batch without tokens are valid empty calls: nothing is written (as for m2rnn_fwd).  An empty
- * sequence of a packed batch has hT = h0. */
+ * T = 0, B = 0 and a batch without tokens are valid empty calls; an empty sequence has hT = h0 (or zeros), also where
+ * all of a call's are empty (unlike m2rnn_fwd, which writes nothing then). */
 int m2rnn_delta_fwd(const m2rnn_delta_params *params, const void *q, const void *k, const void *v, const void *gate,
                     const void *step, const void *h0, const float *alpha, const float *beta, void *y, void *hT,
                     void *ckpt, void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);

@@ -95,6 +95,14 @@ DeltaArgs base_args(const m2rnn_delta_params *p, const void *q, const void *k, c
   a.per_q = p->N / p->Nq; a.per_k = p->N / p->Nk;
   return a;
 }
+// A call without tokens leaves the states as they are: `to` = `from`, or zeros
+int pass_state(const m2rnn_delta_params *p, void *to, const void *from, cudaStream_t s) {
+  if (!aligned16(to) || !aligned16(from)) return M2RNN_ERR_ALIGN;
+  if (!to || to == from || p->B == 0) return M2RNN_OK;
+  const size_t bytes = state_elem(p) * p->B * p->N * p->K * p->V;
+  const cudaError_t e = from ? cudaMemcpyAsync(to, from, bytes, cudaMemcpyDeviceToDevice, s) : cudaMemsetAsync(to, 0, bytes, s);
+  return e == cudaSuccess ? M2RNN_OK : cuda_failed();
+}
 bool empty_call(const m2rnn_delta_params *p) { return p->B == 0 || p->T == 0 || tokens_of(p) == 0; }
 
 // the forward kernels; ckpt: where records (and, with `keep`, states and updates) go
@@ -130,7 +138,7 @@ int m2rnn_delta_fwd(const m2rnn_delta_params *params, const void *q, const void 
                     void *stream) {
   const int rc = check_params(params, false);
   if (rc != M2RNN_OK) return rc;
-  if (empty_call(params)) return M2RNN_OK;
+  if (empty_call(params)) return pass_state(params, hT, h0, static_cast<cudaStream_t>(stream));
   if (!q || !k || !v || !gate || !step || !y) return M2RNN_ERR_NULL;
   if (params->gate_kind == M2RNN_GATE_PSI && (!alpha || !beta)) return M2RNN_ERR_NULL;
   const void *ptrs[] = {q, k, v, gate, step, h0, y, hT, ckpt};
@@ -156,13 +164,7 @@ int m2rnn_delta_bwd(const m2rnn_delta_params *params, const void *q, const void 
   const int rc = check_params(params, false);
   if (rc != M2RNN_OK) return rc;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (empty_call(params)) {      // the only defined output is dh0 = d_hT (or 0)
-    if (!aligned16(dh0) || !aligned16(d_hT)) return M2RNN_ERR_ALIGN;
-    if (!dh0 || params->B == 0) return M2RNN_OK;
-    const size_t bytes = state_elem(params) * params->B * params->N * params->K * params->V;
-    const cudaError_t e = d_hT ? cudaMemcpyAsync(dh0, d_hT, bytes, cudaMemcpyDeviceToDevice, s) : cudaMemsetAsync(dh0, 0, bytes, s);
-    return e == cudaSuccess ? M2RNN_OK : cuda_failed();
-  }
+  if (empty_call(params)) return pass_state(params, dh0, d_hT, s);      // (the only defined output)
   if (!q || !k || !v || !gate || !step || !dy || !dq || !dk || !dv || !dgate || !dstep) return M2RNN_ERR_NULL;
   if (params->gate_kind == M2RNN_GATE_PSI && (!alpha || !beta)) return M2RNN_ERR_NULL;
   const void *ptrs[] = {q, k, v, gate, step, h0, ckpt, dy, d_hT, dq, dk, dv, dgate, dstep, dh0};

@@ -87,3 +87,22 @@ def test_offsets_that_begin_behind_the_first_token(first, Nq, dtype):
     for name, t in out.items():
         assert rel(t[rows], y_r if name == "y" else g_r[name]) <= tol, name
         assert (t[:first] == 3).all() and (t[cu[-1]:] == 3).all(), name
+
+
+@pytest.mark.parametrize("state", [BF, F32], ids=["sbf16", "sf32"])
+@pytest.mark.parametrize("packed", [False, True])
+def test_calls_without_tokens_hand_the_states_on(packed, state):
+    """Every sequence of a call is empty: its final states are the initial ones, as of a single empty sequence."""
+    lead = (0,) if packed else (3, 0)
+    q, gt = torch.zeros(*lead, 2, 32, dtype=BF, device="cuda"), torch.zeros(*lead, 2, dtype=BF, device="cuda")
+    more = dict(cu_seqlens=torch.zeros(4, dtype=torch.int32, device="cuda"), max_seqlen=8) if packed else {}
+    h0 = torch.randn(3, 2, 32, 32, device="cuda").to(state)
+    hT = torch.full_like(h0, math.nan)
+    assert m.m2rnn_delta_fwd(q, q, q, gt, gt, h0, out=dict(hT=hT), **more)[1] is hT and torch.equal(hT, h0)
+    assert torch.equal(m.m2rnn_delta_fwd(q, q, q, gt, gt, h0, **more)[1], h0)
+    assert torch.equal(m.m2rnn_delta_fwd(q, q, q, gt, gt, hT, out=dict(hT=hT), **more)[1], h0)      # in place
+    hT.fill_(math.nan)
+    m.m2rnn_delta_fwd(q, q, q, gt, gt, out=dict(hT=hT), **more)
+    assert (hT == 0).all()
+    g = m.m2rnn_delta_bwd(q, q, q, gt, gt, h0, q, hT + 2, **more)
+    assert (g["dh0"] == 2).all() and g["dh0"].dtype == state
