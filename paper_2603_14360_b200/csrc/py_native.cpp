@@ -241,7 +241,7 @@ Scan scan_params(const Tensor &q, const Tensor &k, const Tensor &v, long gate_ki
     const long most = PyLong_AsLong(n);
     Py_DECREF(n);
     if (PyErr_Occurred()) throw python_error();
-    if (most > INT32_MAX) fail(PyExc_ValueError, "max_seqlen %ld: at most %ld", most, (long)INT32_MAX);
+    if (most < INT32_MIN || most > INT32_MAX) fail(PyExc_ValueError, "max_seqlen %ld: at most %ld", most, (long)INT32_MAX);
     p.T = (int32_t)most;
     p.cu_seqlens = static_cast<const int32_t *>(cu->data_ptr());
     s.lead[0] = q.size(0); s.nlead = 1;

@@ -106,3 +106,14 @@ def test_calls_without_tokens_hand_the_states_on(packed, state):
     assert (hT == 0).all()
     g = m.m2rnn_delta_bwd(q, q, q, gt, gt, h0, q, hT + 2, **more)
     assert (g["dh0"] == 2).all() and g["dh0"].dtype == state
+
+
+@pytest.mark.parametrize("most", [-(1 << 32) + 80, 1 << 31])
+def test_lengths_that_32_bits_do_not_hold(most):
+    """Not cut to what is left of them in 32 bits (80 of the second)."""
+    q, gt = torch.zeros(80, 2, 32, dtype=BF, device="cuda"), torch.zeros(80, 2, dtype=BF, device="cuda")
+    cu = torch.tensor([0, 80], dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError, match="max_seqlen"):
+        m.m2rnn_delta_fwd(q, q, q, gt, gt, cu_seqlens=cu, max_seqlen=most)
+    with pytest.raises(ValueError, match="max_seqlen"):
+        m.m2rnn_fwd(q, q, q, gt.float(), torch.zeros(2, 32, 32, dtype=BF, device="cuda"), cu_seqlens=cu, max_seqlen=most)
