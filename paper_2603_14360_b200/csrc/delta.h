@@ -15,8 +15,10 @@ constexpr int kDeltaChunkF32 = 16;     // (fp32 kernels)
 // What the chains and the gradient kernel need of one chunk of one head (delta_prep.cu):
 //   T, P: 32 x 32 bf16 as 8 x 8 blocks, block (bi, bj) at 128 (4 bi + bj) bytes, its rows 16 bytes each; blocks
 //         above the diagonal of 16 x 16 blocks are not written
+//   TL  : what T's entries lose as bf16: its blocks of 16 x 16 on the diagonal in the places above T's and P's (kRecTLDiag bytes into each),
+//         that below it as four 8 x 8 blocks in a row
 //   vec : eight fp32 values per token, array after array
-constexpr int kRecT = 0, kRecP = 2048, kRecVec = 4096, kRecBytes = 5120;
+constexpr int kRecT = 0, kRecP = 2048, kRecTLDiag = 2 * 128, kRecTL = 4096, kRecVec = 4608, kRecBytes = 5632;
 enum {
   kVecEgk = 0,   // e^g r_k             g: running sum of log a in the chunk, r: 1 / length of the row
   kVecEq = 1,    // s e^g r_q

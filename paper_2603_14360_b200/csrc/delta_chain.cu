@@ -17,8 +17,10 @@
 // (Y after its own chunk's chain: 1 680 cycles a chunk of K = 64 for a warp alone.)  Where SMs have warps to spare, Y is a warp's of its own beside
 // each chain: it finds the chunk's S and U in one of two buffers that the chain fills.  (plan_chain; where they have not, those warps would halve
 // the chains to an SM.)  What is kept for the gradient goes from registers to memory, 128 bytes an instruction.
-// Roundings to bf16: the operands S, X, U (dS, dU, L), the factored e^(g_last - g) U and the like, and T and P.  S itself
-// is held and updated in fp32.
+// Roundings to bf16: the operands S, X, U (dS, dU, L), the factored e^(g_last - g) U and the like, and P.  S itself
+// is held and updated in fp32.  T comes as bf16 and what that leaves, two products: keys that are much alike (a token that is repeated) make its
+// entries near -1, many of one value, and what their roundings add to U, all to the same side, sums up in S (one token throughout, b = 0.98,
+// decay e^-0.002: dstep 1e-1 off, hT 6e-2; with both products 1.4e-2 and 1.8e-2, for 2 to 4 % of a pass).
 // Bound by the chain's latency where an SM has a chain to a scheduler (1 001 tokens, 84 heads of 64 x 16: 16.1 us, 0.45 a chunk; 65 536 tokens,
 // 32 heads of 128 x 128, two chains to an SM: 1 383 us, 0.68 a chunk; 8 x 2 048 tokens, 16 heads of 64 x 64, four: 49.5 us, 0.77), by shared memory's
 // bandwidth where it has more (two to a scheduler: LSU data pipe 83 % busy).
@@ -222,6 +224,19 @@ __device__ __forceinline__ void lower_in(uint32_t (&b)[3][4], uint32_t M, const 
   ldmatrix_x4_t(at + 128 * 8, b[1]);
   ldmatrix_x4_t(at + 128 * 10, b[2]);
 }
+// What T lost as bf16, in a record's three places
+__device__ __forceinline__ void low_t_in(uint32_t (&b)[3][4], uint32_t rec, const Lanes &l) {
+  const uint32_t at = rec + 16 * l.row + 128 * l.mat_lo, diag = at + 512 * l.mat_hi + kRecTLDiag;
+  ldmatrix_x4(diag + kRecT, b[0]);
+  ldmatrix_x4(at + 256 * l.mat_hi + kRecTL, b[1]);
+  ldmatrix_x4(diag + kRecP, b[2]);
+}
+__device__ __forceinline__ void low_in(uint32_t (&b)[3][4], uint32_t rec, const Lanes &l) {
+  const uint32_t at = rec + 16 * l.row + 128 * l.mat_hi, diag = at + 512 * l.mat_lo + kRecTLDiag;
+  ldmatrix_x4_t(diag + kRecT, b[0]);
+  ldmatrix_x4_t(at + 256 * l.mat_lo + kRecTL, b[1]);
+  ldmatrix_x4_t(diag + kRecP, b[2]);
+}
 // acc (16 x 32) += A (16 x 32) . M^T
 __device__ __forceinline__ void mul_lower_t(float (&acc)[4][4], const uint32_t (&A)[2][4], const uint32_t (&b)[3][4]) {
   mma_add(acc[0], A[0], b[0][0], b[0][1]);
@@ -350,12 +365,13 @@ __device__ __forceinline__ int chain_role(const DeltaArgs &a, int nw, bool apart
 
 // Where a chain finds things in a stage
 struct ChainAt { uint32_t v_at, v_mine, r_off; int pv, c; };
-// X from K S, as operands; T
-__device__ __forceinline__ void x_of(const ChainAt &t, const Lanes &l, uint32_t stage, float (&acc)[4][4], uint32_t (&A)[2][4], uint32_t (&T)[3][4]) {
+// X from K S, as operands; T and what it lost as bf16
+__device__ __forceinline__ void x_of(const ChainAt &t, const Lanes &l, uint32_t stage, float (&acc)[4][4], uint32_t (&A)[2][4], uint32_t (&T)[3][4], uint32_t (&TL)[3][4]) {
   const uint32_t vec = stage + t.r_off + kRecVec + 8 * t.c;
   uint32_t vt[2][4];
   rows_in(vt, stage + t.v_at, t.pv);
   lower_t_in(T, stage + t.r_off + kRecT, l);
+  low_t_in(TL, stage + t.r_off, l);
 #pragma unroll
   for (int nt = 0; nt < 4; ++nt) {
     const float2 e = lds64(vec + 128 * kVecEgk + 32 * nt), b = lds64(vec + 128 * kVecBeta + 32 * nt);
@@ -393,10 +409,11 @@ __device__ __forceinline__ void mend(const ChainAt &t, const Lanes &l, uint32_t 
     s_of(kt, f);
     kb.step(acc, f, kt);
   }
-  uint32_t A[2][4], T[3][4];
-  x_of(t, l, stage, acc, A, T);
+  uint32_t A[2][4], T[3][4], TL[3][4];
+  x_of(t, l, stage, acc, A, T, TL);
   const FirstOdd x = take_odd(A, t.c);
   zero(U);
+  mul_lower_t(U, A, TL);
   mul_lower_t(U, A, T);
   pack_a<4>(U, 0, Ub[0]);
   pack_a<4>(U, 1, Ub[1]);
@@ -516,10 +533,11 @@ __global__ void __launch_bounds__(APART == 2 ? 288 : APART ? 224 : 160, APART ? 
       }
     }
     if (WITH) y_rest(t, l, last, y, Ub);
-    uint32_t A[2][4], T[3][4];
-    x_of(t, l, stage, acc, A, T);
+    uint32_t A[2][4], T[3][4], TL[3][4];
+    x_of(t, l, stage, acc, A, T, TL);
     float U[4][4];
     zero(U);
+    mul_lower_t(U, A, TL);
     mul_lower_t(U, A, T);
     Rows<K> rb;
     rb.start(stage, l);
@@ -603,7 +621,7 @@ __global__ void __launch_bounds__(160, 2) delta_chain_bwd_kernel(DeltaArgs a, in
     kb.start(stage, l);
     Rows<K> rb;
     rb.start(qsa, l);
-    uint32_t yt[2][4], A[2][4], T[3][4], P[3][4];
+    uint32_t yt[2][4], A[2][4], T[3][4], TL[3][4], P[3][4];
     rows_in(yt, stage + v_at, pv);
     const float ec = __expf(lds32(stage + r_off + kRecVec + 128 * kVecG + 124));
     {      // s e^g dY
@@ -638,10 +656,12 @@ __global__ void __launch_bounds__(160, 2) delta_chain_bwd_kernel(DeltaArgs a, in
     }
     mul_lower(acc, yt, P);     // (packed accumulators [2kt], [2kt + 1] are the A operand of k-tile kt)
     lower_in(T, stage + r_off + kRecT, l);
+    low_in(TL, stage + r_off, l);
     pack_a<4>(acc, 0, A[0]);
     pack_a<4>(acc, 1, A[1]);
     float L[4][4];
     zero(L);
+    mul_lower(L, A, TL);
     mul_lower(L, A, T);
     rb.start(stage, l);
     float dv[4][4];

@@ -11,7 +11,8 @@
 // slot a feature has does not matter as long as both operands agree, and a row's words are the same as row of A
 // and as column of B.  T is inverted in fp32:
 // the two 16 x 16 blocks on the diagonal by forward substitution, a column a lane (a series of powers of M would
-// cancel digits where keys point the same way), then T_21 = -(T_22 M_21) T_11 with tf32 operands (2^-12 of each, before T is rounded to bf16).
+// cancel digits where keys point the same way), then T_21 = -(T_22 M_21) T_11 with tf32 operands (2^-12 of each).  T goes out as bf16
+// and what that leaves.
 // (65 536 tokens of 32 heads, K = 128, 1.4 GB: 251 us, 5.6 TB/s; with q and k through shared memory, the lengths by FMA and T's last
 // block too 361.)
 #include "delta_common.cuh"
@@ -209,12 +210,18 @@ __global__ void __launch_bounds__(32 * kWarps, 4) delta_prep_kernel(DeltaArgs a,
     }
     __syncwarp();
     uint32_t *Tg = reinterpret_cast<uint32_t *>(rec + kRecT) + lane;
+    auto t_out = [&](int block, int low, float x, float y) {      // as bf16, and what that leaves, `low` bytes into the record
+      const uint32_t high = pack_bf16(x, y);
+      const float2 h = unpack_bf16(high);
+      Tg[32 * block] = high;
+      Tg[(low - kRecT) / 4] = pack_bf16(x - h.x, y - h.y);
+    };
 #pragma unroll
     for (int d = 0; d < 2; ++d)
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         const float2 t = *reinterpret_cast<const float2 *>(Td + d * kTHalf + (8 * (x >> 1) + g) * kPT + 8 * (x & 1) + 2 * c);
-        Tg[(4 * (2 * d + (x >> 1)) + 2 * d + (x & 1)) * 32] = pack_bf16(t.x, t.y);
+        t_out(4 * (2 * d + (x >> 1)) + 2 * d + (x & 1), (d ? kRecP : kRecT) + kRecTLDiag + 128 * (4 * (x >> 1) + (x & 1)), t.x, t.y);
       }
     // W = T_22 M_21; its accumulators are the next product's A operand with columns 2c, 2c + 1 in k slots c, c + 4
     float W[2][4] = {}, Z[2][4] = {};
@@ -249,8 +256,8 @@ __global__ void __launch_bounds__(32 * kWarps, 4) delta_prep_kernel(DeltaArgs a,
     }
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt) {
-      Tg[(4 * 2 + nt) * 32] = pack_bf16(Z[nt][0], Z[nt][1]);
-      Tg[(4 * 3 + nt) * 32] = pack_bf16(Z[nt][2], Z[nt][3]);
+      t_out(4 * 2 + nt, kRecTL + 128 * nt, Z[nt][0], Z[nt][1]);
+      t_out(4 * 3 + nt, kRecTL + 128 * (2 + nt), Z[nt][2], Z[nt][3]);
     }
     __syncwarp();
   }

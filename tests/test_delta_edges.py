@@ -117,3 +117,26 @@ def test_lengths_that_32_bits_do_not_hold(most):
         m.m2rnn_delta_fwd(q, q, q, gt, gt, cu_seqlens=cu, max_seqlen=most)
     with pytest.raises(ValueError, match="max_seqlen"):
         m.m2rnn_fwd(q, q, q, gt.float(), torch.zeros(2, 32, 32, dtype=BF, device="cuda"), cu_seqlens=cu, max_seqlen=most)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("step,decay", [(1.0, 0.0), (0.98, -0.002), (0.7, -0.01), (0.5, -0.05)])
+@pytest.mark.parametrize("cosine", [0.97, 0.994, 0.999, 1.0])
+def test_keys_that_are_nearly_the_same(cosine, step, decay, dtype):
+    """A run of one token, or of tokens much alike: (I + M)^-1 = T has entries near -1 below its diagonal, and what it carries from token to
+    token cancels.
+
+    Bounds: those of test_delta_rule, twice.  With keys of cosine c, M's entries are c b times the decays, at most m = c b in [0, 1], so T's rows
+    hold 1 and m (1 - m)^i, which sum to 2 at most: as much of the roundings of X (of dU in the gradient) comes through it, where keys that
+    point anywhere leave T near I.  (With T itself rounded to bf16, all its entries off to the same side, dstep was 1e-1 off.)"""
+    o = dict(q_scale=1.0, qk_norm=True, norm_eps=1e-6, gate_kind=m.GATE_LOG, step_kind=m.STEP_VALUE)
+    gen = torch.Generator().manual_seed(50)
+    r = lambda *s: torch.randn(*s, generator=gen)  # noqa: E731
+    T, N, K, V = 150, 2, 64, 64
+    base, other = ref.unit(r(1, 1, N, K), 0), r(1, T, N, K)
+    other = ref.unit(other - (other * base).sum(-1, keepdim=True) * base, 0)
+    k = math.sqrt(cosine) * base + math.sqrt(1 - cosine) * other
+    x = [t.to(dtype) for t in (r(1, T, N, K), k, r(1, T, N, V), torch.full((1, T, N), decay), torch.full((1, T, N), step))]
+    H0, d_hT = r(1, N, K, V) * 0.2, r(1, N, K, V) * 0.2
+    errs = forward_and_gradients(x, [t.cuda() for t in x], H0, r(1, T, N, V).to(dtype), d_hT, o)
+    assert max(errs.values()) <= (4e-2 if dtype == BF else 2e-4), errs
