@@ -42,14 +42,10 @@ CSRC = os.path.join(ROOT, "paper_2603_14360_b200", "csrc")
 
 
 def kernel_source_digest(cu_file: str) -> str:
-    """Digest of a kernel's translation unit and the headers of its directory: the table's rows are
+    """Digest of a kernel's translation unit and the headers that it includes: the table's rows are
     valid for the sources they were captured from, not after a change."""
-    import hashlib
-    h = hashlib.sha256()
-    names = [cu_file] + sorted(f for f in os.listdir(CSRC) if f.endswith((".cuh", ".h")))
-    for f in names:
-        h.update(open(os.path.join(CSRC, f), "rb").read())
-    return h.hexdigest()[:16]
+    from paper_2603_14360_b200 import ncu_traffic
+    return ncu_traffic.source_digest(cu_file)
 
 
 def profiled_traffic(workload: str, units: int):

@@ -103,6 +103,8 @@ cudaError_t launch_delta_chain_bwd(const DeltaArgs &a, cudaStream_t s);
 struct GradPlan { int heads, ctas; };
 GradPlan delta_grad_plan(const m2rnn_delta_params *p, size_t slots);      // delta_grad.cu
 cudaError_t launch_delta_grad(const DeltaArgs &a, cudaStream_t s);
+// launch_reduce_heads (reduce.cu); of a packed batch (cu, with B and T) only rows of tokens that belong to a sequence are written
+cudaError_t launch_reduce_heads_of(const float *part, void *out, int io_dtype, size_t BT, int N, int Ng, int K, const int32_t *cu, int B, int T, cudaStream_t s);
 cudaError_t launch_delta_fwd_f32(const DeltaArgs &a, cudaStream_t s);     // delta_f32.cu
 cudaError_t launch_delta_bwd_f32(const DeltaArgs &a, cudaStream_t s);
 

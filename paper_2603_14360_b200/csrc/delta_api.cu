@@ -197,8 +197,8 @@ int m2rnn_delta_bwd(const m2rnn_delta_params *params, const void *q, const void 
     if (e == cudaSuccess) e = launch_delta_grad(a, s);
   }
   const size_t tokens = tokens_of(params);
-  if (e == cudaSuccess && a.dq_part) e = launch_reduce_heads(a.dq_part, dq, params->io_dtype, tokens, a.shares, params->Nq, params->K, s, a.cu, a.B, a.T);
-  if (e == cudaSuccess && a.dk_part) e = launch_reduce_heads(a.dk_part, dk, params->io_dtype, tokens, a.shares, params->Nk, params->K, s, a.cu, a.B, a.T);
+  if (e == cudaSuccess && a.dq_part) e = launch_reduce_heads_of(a.dq_part, dq, params->io_dtype, tokens, a.shares, params->Nq, params->K, a.cu, a.B, a.T, s);
+  if (e == cudaSuccess && a.dk_part) e = launch_reduce_heads_of(a.dk_part, dk, params->io_dtype, tokens, a.shares, params->Nk, params->K, a.cu, a.B, a.T, s);
   return e == cudaSuccess ? M2RNN_OK : cuda_failed();
 }
 

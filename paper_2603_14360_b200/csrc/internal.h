@@ -186,8 +186,7 @@ cudaError_t launch_decode_tc_bf16(const ScanArgs &a, cudaStream_t s);  // decode
 // reductions shared by both paths (reduce.cu)
 cudaError_t launch_reduce_dW(const float *dW_part, float *dW, int B, int N, int V, cudaStream_t s);
 cudaError_t launch_reduce_slabs(const float *part, void *out, int io_dtype, int R, size_t n, cudaStream_t s);
-// cu (with B and T): of a packed batch only rows of tokens that belong to a sequence are written
 cudaError_t launch_reduce_heads(const float *part, void *out, int io_dtype, size_t BT, int N,
-                                int Ng, int K, cudaStream_t s, const int32_t *cu = nullptr, int B = 0, int T = 0);
+                                int Ng, int K, cudaStream_t s);
 
 }  // namespace m2rnn

@@ -1,5 +1,6 @@
 // Second-stage reductions of the backward pass, in a fixed order so results repeat bit for bit
 // (the paper's Algorithm 2 uses atomic adds for these sums).
+#include "delta.h"
 #include "device_common.cuh"
 #include "internal.h"
 
@@ -116,8 +117,10 @@ cudaError_t launch_reduce_dW(const float *dW_part, float *dW, int B, int N, int 
   return cudaGetLastError();
 }
 
-cudaError_t launch_reduce_heads(const float *part, void *out, int io_dtype, size_t BT, int N, int Ng,
-                                int K, cudaStream_t s, const int32_t *cu, int B, int T) {
+cudaError_t launch_reduce_heads(const float *part, void *out, int io_dtype, size_t BT, int N, int Ng, int K, cudaStream_t s) {
+  return launch_reduce_heads_of(part, out, io_dtype, BT, N, Ng, K, nullptr, 0, 0, s);
+}
+cudaError_t launch_reduce_heads_of(const float *part, void *out, int io_dtype, size_t BT, int N, int Ng, int K, const int32_t *cu, int B, int T, cudaStream_t s) {
   const size_t rows = BT * Ng;
   const int per = N / Ng, K4 = K / 4;
   const unsigned grid = (unsigned)((rows * K4 + 255) / 256);

@@ -27,9 +27,22 @@ HEADER = ("# DRAM traffic of one launch of each workload's dominant kernel, from
           "# workload[:kernel of a step made of several]  kernel  source  dram_bytes_per_launch  units_captured (token-heads; tokens for in_conv, out_norm)  source_digest  ncu_dram_read  ncu_dram_write  launches\n")
 
 
+def sources_of(cu_file: str) -> list:
+    """A translation unit and what it includes of its directory, directly or not."""
+    todo, seen = [cu_file], {cu_file}
+    while todo:
+        text = open(os.path.join(CSRC, todo.pop())).read()
+        for f in re.findall(r'^\s*#\s*include\s*"([^"]+)"', text, re.M):
+            if f not in seen and os.path.exists(os.path.join(CSRC, f)):
+                seen.add(f)
+                todo.append(f)
+    return [cu_file] + sorted(seen - {cu_file})
+
+
 def source_digest(cu_file: str) -> str:
+    """Digest of those files: a row is void once one of them has changed, not when the directory gets a header that the kernel never sees."""
     h = hashlib.sha256()
-    for f in [cu_file] + sorted(x for x in os.listdir(CSRC) if x.endswith((".cuh", ".h"))):
+    for f in sources_of(cu_file):
         h.update(open(os.path.join(CSRC, f), "rb").read())
     return h.hexdigest()[:16]
 
