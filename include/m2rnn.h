@@ -291,8 +291,10 @@ int m2rnn_conv_silu_bwd(int32_t B, int32_t T, int32_t C, int32_t io_dtype, const
  * M2RNN_GATE_LOGIT, M2RNN_GATE_PSI as above.  (M2RNN_GATE_VALUE is refused: the kernels and the gradient work on log a.)
  * b_t comes from the step tensor by step_kind.  A token with a = 1 and b = 0 leaves the state as it is.
  * With M2RNN_BF16 the sequence is taken in chunks of 32 tokens whose products run on tensor cores: bf16 operands (the
- * state's included), fp32 accumulation, the state itself held in fp32.  Outputs of fp32 type (a state_dtype of
- * M2RNN_F32) then carry the error of those operands, some 3e-3 of their norm.  With M2RNN_F32 everything is fp32 FMA.
+ * state's included), fp32 accumulation, the state itself held in fp32.  Results, those of fp32 type (a state_dtype of
+ * M2RNN_F32) too, then carry the error of those operands: where keys point anywhere 4e-3 of their norm, 5e-3 with
+ * gradients; where they are much alike up to 1e-2 and 2e-2 (cosines of 0.97 to 1, b near 1, slow decays: what a token
+ * adds is a small difference then).  With M2RNN_F32 everything is fp32 FMA (1e-6, then too).
  * What is not finite stays behind its token: no y of an earlier one, of another head or sequence changes (in q: only
  * that token's y; in v: only that column).  The gradients of a sequence with such a value, in dy or d_hT too, are
  * undefined.
