@@ -21,8 +21,8 @@
 // is held and updated in fp32.  T comes as bf16 and what that leaves, two products: keys that are much alike (a token that is repeated) make its
 // entries near -1, many of one value, and what their roundings add to U, all to the same side, sums up in S (one token throughout, b = 0.98,
 // decay e^-0.002: dstep 1e-1 off, hT 6e-2; with both products 1.4e-2 and 1.8e-2, for 2 to 4 % of a pass).
-// Bound by the chain's latency where an SM has a chain to a scheduler (1 001 tokens, 84 heads of 64 x 16: 16.1 us, 0.45 a chunk; 65 536 tokens,
-// 32 heads of 128 x 128, two chains to an SM: 1 383 us, 0.68 a chunk; 8 x 2 048 tokens, 16 heads of 64 x 64, four: 49.5 us, 0.77), by shared memory's
+// Bound by the chain's latency where an SM has a chain to a scheduler (1 001 tokens, 84 heads of 64 x 16: 16.9 us, 0.48 a chunk; 65 536 tokens,
+// 32 heads of 128 x 128, two chains to an SM: 1 417 us, 0.69 a chunk; 8 x 2 048 tokens, 16 heads of 64 x 64, four: 51.9 us, 0.81), by shared memory's
 // bandwidth where it has more (two to a scheduler: LSU data pipe 83 % busy).
 #include <algorithm>
 
@@ -695,6 +695,7 @@ __global__ void __launch_bounds__(160, 2) delta_chain_bwd_kernel(DeltaArgs a, in
   if (a.dh0) state_out<K>(S, a.dh0, st_at, a.state_bf16, V, g, c);
 }
 
+// (The figures in here were taken with T in one part; the second adds 2 to 4 % to either side of each.)
 // 16-column warps of a CTA: four (they share the copies of k, q and the records), two or one where that leaves a quarter fewer chains to
 // the SM that has the most: chains of an SM share its shared memory's bandwidth (65 536 tokens, 32 heads of 128 x 128: 64 CTAs of four
 // 2 354 us, 128 of two 1 576, both with Y in the chains).
@@ -709,7 +710,8 @@ ChainPlan plan_chain(const DeltaArgs &a, bool with_y) {
   }
   p.slabs = cols / p.nw;
   // Two CTAs to an SM where there are that many, but above K = 64 one: four chains of K = 128 take 1.5 us a chunk, eight 2.9, and a batch
-  // is done no sooner than its longest sequence (12 of up to 4 000 tokens, 16 heads: 370 us with two, 266 with one).
+  // is done no sooner than its longest sequence (12 of up to 4 000 tokens, 16 heads: 370 us with two, 266 with one).  These are CTAs of four
+  // chains; those of one (V = 16) follow the rule too, which was not measured where there are more of them than SMs.
   const bool one = a.K > 64;
   const long long per = (units * p.slabs + sms - 1) / sms;
   // Y in warps of their own where an SM has one CTA, or up to four of one chain (2 001 tokens a sequence, us without and with): 84 heads of 128 x 16

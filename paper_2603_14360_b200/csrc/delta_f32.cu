@@ -8,8 +8,8 @@
 //          chunk's rows in shared memory (stages that a warp of its own fills by cp.async); few columns to a CTA where there are few units.
 //   grad : a CTA a chunk of one head, everything of it in shared memory; four tokens' entries of a feature to a thread.
 // States of chunks are kept column after column, [V][K], so that a column's lanes write contiguous floats.
-// Bound by the latency of FMAs, shuffles and shared memory: 2 x 512 tokens of 8 heads of 64 x 64 take 10.6 (prep), 42.7 and 38.6 (chains, 1.3 us
-// and 1.2 a chunk) and 33.3 us (grad, two CTAs to an SM), against 2.7 for the bytes.
+// Bound by the latency of FMAs, shuffles and shared memory: 2 x 512 tokens of 8 heads of 64 x 64 take 11.2 (prep), 42.2 and 38.3 (chains, 1.3 us
+// and 1.2 a chunk) and 33.1 us (grad, two CTAs to an SM), against 2.7 for the bytes.
 #include "delta_common.cuh"
 
 namespace m2rnn {

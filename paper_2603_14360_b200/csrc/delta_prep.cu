@@ -13,8 +13,8 @@
 // the two 16 x 16 blocks on the diagonal by forward substitution, a column a lane (a series of powers of M would
 // cancel digits where keys point the same way), then T_21 = -(T_22 M_21) T_11 with tf32 operands (2^-12 of each).  T goes out as bf16
 // and what that leaves.
-// (65 536 tokens of 32 heads, K = 128, 1.4 GB: 251 us, 5.6 TB/s; with q and k through shared memory, the lengths by FMA and T's last
-// block too 361.)
+// (65 536 tokens of 32 heads, K = 128, 1.45 GB: 270 us, 5.4 TB/s; a form with q and k through shared memory, the lengths by FMA and T's
+// last block too took 361.)
 #include "delta_common.cuh"
 
 namespace m2rnn {
